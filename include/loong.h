@@ -268,6 +268,61 @@ LOONG_API int loong_reduce_replicas(int64_t heads, int32_t rep, int64_t elems_pe
                                     void* stream);
 
 /*
+ * Before the first step and after the last: the norm of every query and key head and the rotation by position, in one
+ * pass over q and k, and their gradient.  For every row x of head_dim elements at position p
+ *   n_j = w_j x_j / sqrt(mean(x^2) + eps)                       (with LOONG_QK_NORM; n = x without)
+ *   y_a = n_a cos(p f_i) - n_b sin(p f_i),  y_b = n_a sin(p f_i) + n_b cos(p f_i),  i = 0 .. rot_dim/2 - 1
+ * for the pairs (a, b) = (i, i + rot_dim/2), or (2i, 2i + 1) with LOONG_ROPE_INTERLEAVED; elements from rot_dim on are
+ * not rotated.  f_i = inv_freq[i], radians per position (device, fp32; may be NULL if rot_dim is 0); p f_i is formed in
+ * 64 bits.  w: `q_weight`, `k_weight`, device, fp32 [head_dim] each, NULL for ones.
+ * The position of token i of batch element b: positions[b * len + i] (device, int32) if `positions` is given; else, with
+ * chunk_len > 0, its place in the whole sequence when the tokens are a zigzag pair of chunks (len == 2 * chunk_len;
+ * q_chunk of loong_zigzag_mask); else i.
+ */
+#define LOONG_QK_NORM          4096   /* rope, append: the norm is applied before the rotation */
+#define LOONG_ROPE_INTERLEAVED 8192   /* rope, append: neighbouring elements are rotated together */
+
+typedef struct loong_rope_desc {
+  int32_t batch;
+  int32_t n_q_heads;      /* 0: there is no q (its pointers may be NULL) */
+  int32_t n_kv_heads;     /* 0: there is no k */
+  int32_t head_dim;       /* a multiple of 16, at most 256 */
+  int32_t rot_dim;        /* a multiple of 16, 0 .. head_dim */
+  int32_t len;            /* tokens per batch element */
+  int32_t chunk_len;      /* 0, or len / 2: see above */
+  int32_t chunk[2];       /* global chunk ids of tokens [0,c) and [c,2c) */
+  int32_t dtype;          /* LOONG_BF16 | LOONG_FP32 | LOONG_FP16: q, k, their rotated form and their gradients dq, dk */
+  float   eps;            /* LOONG_QK_NORM: finite, not negative */
+  int32_t flags;          /* LOONG_QK_NORM | LOONG_ROPE_INTERLEAVED */
+  int64_t q_stride[3];    /* batch, head, token strides (elements) of q and dq */
+  int64_t k_stride[3];    /* of k and dk */
+  int64_t q_out_stride[3];/* of q_out and its gradient d_q_out */
+  int64_t k_out_stride[3];/* of k_out and its gradient d_k_out */
+} loong_rope_desc;
+
+/* q_out, k_out <- the rows of q, k, normed and rotated; rounded to dtype once, at the end.  In place (q_out == q with equal
+ * strides, likewise k) is fine; otherwise inputs and outputs must not overlap. */
+LOONG_API int loong_qk_rope_fwd(const loong_rope_desc* desc, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                                const float* inv_freq, const int32_t* positions, void* q_out, void* k_out, void* stream);
+
+/*
+ * The gradient: q, k are the forward's inputs; d_q_out, d_k_out the fp32 gradients of its outputs, as the attention steps leave
+ * them in dq and dk.  dq, dk (dtype) are overwritten with the gradients of q and k; dq_weight, dk_weight (fp32
+ * [head_dim], overwritten; NULL: not wanted) with those of the weights, summed over all rows in a fixed order: bit-reproducible.
+ * Where a weight's gradient is wanted, `workspace` is device memory of the caller's, 16-byte aligned, of
+ * loong_qk_rope_workspace_bytes(desc) bytes; it may hold anything on entry; calls that share one must be ordered on one
+ * stream.  Without LOONG_QK_NORM there are no weights: their gradients' pointers must be NULL.
+ * Errors of both calls: LOONG_E_NULL, LOONG_E_SHAPE, LOONG_E_UNSUPPORTED, LOONG_E_ALIGN (tensors 16-byte aligned, strides multiples of
+ * 16 bytes), LOONG_E_DTYPE.
+ */
+LOONG_API int loong_qk_rope_bwd(const loong_rope_desc* desc, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                                const float* inv_freq, const int32_t* positions, const float* d_q_out, const float* d_k_out,
+                                void* dq, void* dk, float* dq_weight, float* dk_weight, void* workspace, int64_t workspace_bytes,
+                                void* stream);
+/* Host-only; the answer depends on the current device as that of loong_workspace_bytes does. */
+LOONG_API int loong_qk_rope_workspace_bytes(const loong_rope_desc* desc, int64_t* bytes);
+
+/*
  * Performance model of 2D-Attention (paper: Sec. "Performance Analysis": "Computation
  * Analysis", "P2P Communication Analysis", "SeqAlltoAll Communication Analysis").  Host only.
  * Inputs: sequence length S and hidden size D (elements), H query heads, H_kv key/value

@@ -19,6 +19,7 @@ FUSE_MERGE, ACCUM_DKV, COMPUTE_DELTA, BWD_ONLY_DKV, BWD_ONLY_DQ = 1, 2, 4, 8, 16
 OVERWRITE_DQ, WORKSPACE_CLEAN = 32, 64
 WORKSPACE_HEAD = 65536   # bytes of a workspace that WORKSPACE_CLEAN speaks of
 KEY_SPLITS_SHIFT = 8
+QK_NORM, ROPE_INTERLEAVED = 4096, 8192
 
 
 def key_splits(n: int) -> int:
@@ -32,6 +33,7 @@ EXPORTS = (
     "loong_last_error", "loong_version", "loong_mfma_probe", "loong_cost_model", "loong_cost_search",
     "loong_permute_rows", "loong_reduce_replicas", "loong_workspace_bytes", "loong_attn_step_bwd_static",
     "loong_attn_steps_fwd", "loong_attn_steps_bwd", "loong_workspace_bytes_steps",
+    "loong_qk_rope_fwd", "loong_qk_rope_bwd", "loong_qk_rope_workspace_bytes",
 )
 
 
@@ -49,6 +51,16 @@ class StepDesc(C.Structure):
         ("q_chunk", C.c_int32 * 2), ("kv_chunk", C.c_int32 * 2),
         ("causal", C.c_int32), ("dtype", C.c_int32), ("softmax_scale", C.c_float), ("flags", C.c_int32),
         ("q_stride", C.c_int64 * 3), ("kv_stride", C.c_int64 * 3), ("o_stride", C.c_int64 * 3),
+    ]
+
+
+class RopeDesc(C.Structure):
+    """Mirror of loong_rope_desc."""
+    _fields_ = [
+        ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("rot_dim", C.c_int32), ("len", C.c_int32), ("chunk_len", C.c_int32), ("chunk", C.c_int32 * 2),
+        ("dtype", C.c_int32), ("eps", C.c_float), ("flags", C.c_int32), ("q_stride", C.c_int64 * 3),
+        ("k_stride", C.c_int64 * 3), ("q_out_stride", C.c_int64 * 3), ("k_out_stride", C.c_int64 * 3),
     ]
 
 
@@ -101,6 +113,9 @@ lib.loong_mfma_probe.argtypes = [_i32, _i32, _vp, _vp, _vp]
 lib.loong_workspace_bytes.argtypes = [C.POINTER(StepDesc), C.POINTER(C.c_int64)]
 lib.loong_permute_rows.argtypes = [C.POINTER(_i64), C.POINTER(_i64), C.POINTER(_i64), _i64, _vp, _vp, _vp]
 lib.loong_reduce_replicas.argtypes = [_i64, _i32, _i64, _vp, _vp, _vp]
+lib.loong_qk_rope_fwd.argtypes = [C.POINTER(RopeDesc)] + [_vp] * 9
+lib.loong_qk_rope_bwd.argtypes = [C.POINTER(RopeDesc)] + [_vp] * 13 + [_i64, _vp]
+lib.loong_qk_rope_workspace_bytes.argtypes = [C.POINTER(RopeDesc), C.POINTER(C.c_int64)]
 lib.loong_cost_model.argtypes = [C.POINTER(CostIn), C.POINTER(CostOut)]
 lib.loong_cost_search.argtypes = [C.POINTER(CostIn), _i32, _i32, C.POINTER(CostIn), C.POINTER(CostOut)]
 lib.loong_last_error.restype = C.c_char_p
@@ -119,6 +134,38 @@ def _ptr(x):
     if isinstance(x, int):
         return x
     return x.data_ptr()
+
+
+_torch_types = {}   # torch's of each dtype code
+
+
+def _tensors(*named):
+    """Device pointers of (name, tensor, dtype code or torch dtype), after the check that a kernel on the current device may
+    read them as what the call says they are; ints and None are passed through."""
+    ptrs, dev = [], None
+    for name, x, dtype in named:
+        if x is None or isinstance(x, int):
+            ptrs.append(x)
+            continue
+        if dev is None:
+            import torch
+            dev = torch.cuda.current_device() if torch.cuda.is_available() else -2
+            if not _torch_types:
+                _torch_types.update({BF16: torch.bfloat16, FP32: torch.float32, FP16: torch.float16, "i32": torch.int32})
+        if x.get_device() != dev:
+            raise ValueError(f"{name} is on {x.device}, not on the current GPU")
+        if x.dtype is not _torch_types.get(dtype, x.dtype):   # (an unknown code is the library's to refuse)
+            raise TypeError(f"{name} is {x.dtype}, not {_torch_types[dtype]}")
+        ptrs.append(x.data_ptr())
+    return ptrs
+
+
+def _workspace(x, n_bytes):
+    """(pointer, bytes) of a workspace tensor, or of a pointer with its size."""
+    (ptr,) = _tensors(("workspace", x, None))
+    if n_bytes is None:
+        n_bytes = 0 if x is None or isinstance(x, int) else x.numel() * x.element_size()
+    return ptr, n_bytes
 
 
 def pointer_array(addresses):
@@ -311,3 +358,45 @@ def init_running(rows: int, head_dim: int, out, lse, stream=None):
 
 def finalize_out(rows: int, head_dim: int, out, o, dtype: int, stream=None):
     _check(lib.loong_finalize_out(rows, head_dim, _ptr(out), _ptr(o), dtype, _stream(stream)))
+
+
+def make_rope_desc(*, batch, n_q_heads, n_kv_heads, head_dim, len, dtype, rot_dim=None, chunk_len=0, chunk=(0, 0), eps=0.0, flags=0,
+                   q_stride=None, k_stride=None, q_out_stride=None, k_out_stride=None) -> RopeDesc:
+    """Descriptor of qk_rope_fwd and qk_rope_bwd: whole heads rotated and contiguous [batch, head, token, head_dim] strides
+    unless given."""
+    def contig(h):
+        return (h * len * head_dim, len * head_dim, head_dim)
+    d = RopeDesc()
+    d.batch, d.n_q_heads, d.n_kv_heads, d.head_dim = batch, n_q_heads, n_kv_heads, head_dim
+    d.rot_dim, d.len, d.chunk_len = head_dim if rot_dim is None else rot_dim, len, chunk_len
+    d.chunk[:] = chunk
+    d.dtype, d.eps, d.flags = dtype, eps, flags
+    d.q_stride[:] = q_stride or contig(n_q_heads)
+    d.k_stride[:] = k_stride or contig(n_kv_heads)
+    d.q_out_stride[:] = q_out_stride or contig(n_q_heads)
+    d.k_out_stride[:] = k_out_stride or contig(n_kv_heads)
+    return d
+
+
+def qk_rope_fwd(desc: RopeDesc, q, k, q_weight, k_weight, inv_freq, positions, q_out, k_out, stream=None):
+    """loong_qk_rope_fwd; weights, positions (and what of q, k is not there) may be None."""
+    t = desc.dtype
+    _check(lib.loong_qk_rope_fwd(C.byref(desc), *_tensors(
+        ("q", q, t), ("k", k, t), ("q_weight", q_weight, FP32), ("k_weight", k_weight, FP32), ("inv_freq", inv_freq, FP32),
+        ("positions", positions, "i32"), ("q_out", q_out, t), ("k_out", k_out, t)), _stream(stream)))
+
+
+def qk_rope_workspace_bytes(desc: RopeDesc) -> int:
+    n = C.c_int64(0)
+    _check(lib.loong_qk_rope_workspace_bytes(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def qk_rope_bwd(desc: RopeDesc, q, k, q_weight, k_weight, inv_freq, positions, d_q_out, d_k_out, dq, dk, dq_weight=None, dk_weight=None,
+                workspace=None, workspace_bytes=None, stream=None):
+    """loong_qk_rope_bwd; `workspace` as in attn_step_bwd."""
+    t = desc.dtype
+    _check(lib.loong_qk_rope_bwd(C.byref(desc), *_tensors(
+        ("q", q, t), ("k", k, t), ("q_weight", q_weight, FP32), ("k_weight", k_weight, FP32), ("inv_freq", inv_freq, FP32),
+        ("positions", positions, "i32"), ("d_q_out", d_q_out, FP32), ("d_k_out", d_k_out, FP32), ("dq", dq, t), ("dk", dk, t),
+        ("dq_weight", dq_weight, FP32), ("dk_weight", dk_weight, FP32)), *_workspace(workspace, workspace_bytes), _stream(stream)))
