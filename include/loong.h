@@ -323,6 +323,68 @@ LOONG_API int loong_qk_rope_bwd(const loong_rope_desc* desc, const void* q, cons
 LOONG_API int loong_qk_rope_workspace_bytes(const loong_rope_desc* desc, int64_t* bytes);
 
 /*
+ * A paged cache and the attention that reads it.  k_cache, v_cache are [n_pages, n_kv_heads, page_size, head_dim] by the strides
+ * of cache_stride (page, head, slot); sequence b holds its keys 0 .. kv_len[b] - 1 in order, key j in slot j % page_size of
+ * page page_table[b * table_stride + j / page_size].  Pages may be shared (a common prefix) as long as one call
+ * writes no slot twice.  The new tokens of all sequences lie one behind the other, [n_tokens, head, head_dim]: those of
+ * sequence b are rows seq_start[b] .. seq_start[b + 1] - 1 and are its LAST keys (kv_len counts them); rows before
+ * seq_start[0] or from seq_start[n_seqs] on belong to none and are left as they are everywhere.  seq_start (n_seqs + 1 numbers),
+ * kv_len and page_table are int32 in DEVICE memory and are read by the kernels, not by the call: a captured call follows
+ * them from replay to replay.  What they hold is checked there: seq_start is taken within [0, n_tokens] (and must not
+ * decrease: rows may be left as they are if it does), a negative kv_len as 0, and pages outside [0, n_pages) or past max_pages are not accessed (append: nothing is stored; attention: rows that
+ * would see such a page get NaN).
+ */
+typedef struct loong_paged_desc {
+  int32_t n_seqs;
+  int32_t n_tokens;       /* rows of q, k, v, out, lse */
+  int32_t max_new;        /* attention: no sequence has more new tokens; rows past that are left as they are.  (1 when decoding;
+                             n_tokens if nothing better is known) */
+  int32_t n_q_heads;      /* q head h reads kv head h / (n_q_heads / n_kv_heads) */
+  int32_t n_kv_heads;
+  int32_t head_dim;       /* 64 or 128 */
+  int32_t dtype;          /* LOONG_BF16 | LOONG_FP16 */
+  int32_t n_pages, page_size, max_pages;   /* pages in the cache; slots of a page; pages a row of page_table has */
+  int32_t rot_dim;        /* append: as in loong_rope_desc */
+  float   eps;            /* append: as in loong_rope_desc */
+  int32_t causal;         /* attention: new token i of n sees keys 0 .. kv_len - n + i; 0: all kv_len (another rank's
+                             part of a longer context, an encoder's states) */
+  float   softmax_scale;  /* attention */
+  int32_t flags;          /* append: LOONG_QK_NORM, LOONG_ROPE_INTERLEAVED; attention: LOONG_WORKSPACE_CLEAN */
+  int64_t table_stride;   /* elements */
+  int64_t q_stride[2];    /* token, head strides (elements) of q */
+  int64_t kv_stride[2];   /* append: of the new k and v */
+  int64_t o_stride[2];    /* append: of q_out; attention: of out and o */
+  int64_t cache_stride[3];/* page, head, slot strides of k_cache and v_cache */
+} loong_paged_desc;
+
+/*
+ * The new tokens' keys and values into the cache: k normed and rotated as by loong_qk_rope_fwd, v as it is, at slot
+ * kv_len - n + i for new token i of n; and q, normed and rotated likewise, into q_out (q and q_out both NULL: keys and values only).
+ * The rotation's position is that slot, or positions[token] if `positions` (device, int32 [n_tokens]) is given.  A token
+ * whose slot is negative is not stored.  q_out == q with equal strides is fine.
+ */
+LOONG_API int loong_paged_append(const loong_paged_desc* desc, const void* q, const void* k, const void* v, const float* q_weight,
+                                 const float* k_weight, const float* inv_freq, const int32_t* positions, const int32_t* seq_start,
+                                 const int32_t* kv_len, const int32_t* page_table, void* q_out, void* k_cache, void* v_cache,
+                                 void* stream);
+
+/*
+ * Attention of the new tokens over the cache: for every new token i of n of a sequence and every q head, softmax(scale q k^T) v over
+ * the keys it sees (see `causal`), rows that see none giving out = 0, lse = -inf.  `out` (fp32) and `o` (dtype, rounded once from
+ * the fp32 result) have o_stride; either may be NULL, not both; lse, fp32 contiguous [n_tokens, n_q_heads], is the natural-log sum of
+ * exp.  With contiguous `out`, results over several parts of a context are merged by loong_lse_merge with rows = n_tokens * n_q_heads.
+ * Long contexts of few rows are shared by several workgroups; which, follows from the lengths, and the last to arrive adds
+ * their results up in order: the same lengths give the same bits.  Their results and counters live in `workspace`, 16-byte aligned, of
+ * loong_paged_workspace_bytes(desc) bytes (that may be 0: then it may be NULL); contents, order and LOONG_WORKSPACE_CLEAN as for
+ * loong_attn_step_bwd.  What a masked key or value holds, be it infinite or NaN, has no effect.
+ */
+LOONG_API int loong_paged_attn(const loong_paged_desc* desc, const void* q, const void* k_cache, const void* v_cache,
+                               const int32_t* seq_start, const int32_t* kv_len, const int32_t* page_table, float* out, void* o,
+                               float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+/* Host-only; the answer depends on the current device as that of loong_workspace_bytes does. */
+LOONG_API int loong_paged_workspace_bytes(const loong_paged_desc* desc, int64_t* bytes);
+
+/*
  * Performance model of 2D-Attention (paper: Sec. "Performance Analysis": "Computation
  * Analysis", "P2P Communication Analysis", "SeqAlltoAll Communication Analysis").  Host only.
  * Inputs: sequence length S and hidden size D (elements), H query heads, H_kv key/value

@@ -34,6 +34,7 @@ EXPORTS = (
     "loong_permute_rows", "loong_reduce_replicas", "loong_workspace_bytes", "loong_attn_step_bwd_static",
     "loong_attn_steps_fwd", "loong_attn_steps_bwd", "loong_workspace_bytes_steps",
     "loong_qk_rope_fwd", "loong_qk_rope_bwd", "loong_qk_rope_workspace_bytes",
+    "loong_paged_append", "loong_paged_attn", "loong_paged_workspace_bytes",
 )
 
 
@@ -61,6 +62,16 @@ class RopeDesc(C.Structure):
         ("rot_dim", C.c_int32), ("len", C.c_int32), ("chunk_len", C.c_int32), ("chunk", C.c_int32 * 2),
         ("dtype", C.c_int32), ("eps", C.c_float), ("flags", C.c_int32), ("q_stride", C.c_int64 * 3),
         ("k_stride", C.c_int64 * 3), ("q_out_stride", C.c_int64 * 3), ("k_out_stride", C.c_int64 * 3),
+    ]
+
+
+class PagedDesc(C.Structure):
+    """Mirror of loong_paged_desc."""
+    _fields_ = [(n, C.c_int32) for n in (
+        "n_seqs", "n_tokens", "max_new", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "n_pages", "page_size", "max_pages",
+        "rot_dim")] + [
+        ("eps", C.c_float), ("causal", C.c_int32), ("softmax_scale", C.c_float), ("flags", C.c_int32), ("table_stride", C.c_int64),
+        ("q_stride", C.c_int64 * 2), ("kv_stride", C.c_int64 * 2), ("o_stride", C.c_int64 * 2), ("cache_stride", C.c_int64 * 3),
     ]
 
 
@@ -116,6 +127,9 @@ lib.loong_reduce_replicas.argtypes = [_i64, _i32, _i64, _vp, _vp, _vp]
 lib.loong_qk_rope_fwd.argtypes = [C.POINTER(RopeDesc)] + [_vp] * 9
 lib.loong_qk_rope_bwd.argtypes = [C.POINTER(RopeDesc)] + [_vp] * 13 + [_i64, _vp]
 lib.loong_qk_rope_workspace_bytes.argtypes = [C.POINTER(RopeDesc), C.POINTER(C.c_int64)]
+lib.loong_paged_append.argtypes = [C.POINTER(PagedDesc)] + [_vp] * 14
+lib.loong_paged_attn.argtypes = [C.POINTER(PagedDesc)] + [_vp] * 10 + [_i64, _vp]
+lib.loong_paged_workspace_bytes.argtypes = [C.POINTER(PagedDesc), C.POINTER(C.c_int64)]
 lib.loong_cost_model.argtypes = [C.POINTER(CostIn), C.POINTER(CostOut)]
 lib.loong_cost_search.argtypes = [C.POINTER(CostIn), _i32, _i32, C.POINTER(CostIn), C.POINTER(CostOut)]
 lib.loong_last_error.restype = C.c_char_p
@@ -400,3 +414,49 @@ def qk_rope_bwd(desc: RopeDesc, q, k, q_weight, k_weight, inv_freq, positions, d
         ("q", q, t), ("k", k, t), ("q_weight", q_weight, FP32), ("k_weight", k_weight, FP32), ("inv_freq", inv_freq, FP32),
         ("positions", positions, "i32"), ("d_q_out", d_q_out, FP32), ("d_k_out", d_k_out, FP32), ("dq", dq, t), ("dk", dk, t),
         ("dq_weight", dq_weight, FP32), ("dk_weight", dk_weight, FP32)), *_workspace(workspace, workspace_bytes), _stream(stream)))
+
+
+def make_paged_desc(*, n_seqs, n_tokens, n_q_heads, n_kv_heads, head_dim, dtype, n_pages, page_size, max_pages, max_new=None, rot_dim=None,
+                    eps=0.0, causal=True, softmax_scale=None, flags=0, table_stride=None, q_stride=None, kv_stride=None, o_stride=None,
+                    cache_stride=None) -> PagedDesc:
+    """Descriptor of paged_append and paged_attn: new tokens contiguous [token, head, head_dim], the cache contiguous
+    [page, head, slot, head_dim], whole heads rotated and a scale of 1/sqrt(head_dim) unless given."""
+    d = PagedDesc()
+    d.n_seqs, d.n_tokens, d.max_new = n_seqs, n_tokens, n_tokens if max_new is None else max_new
+    d.n_q_heads, d.n_kv_heads, d.head_dim, d.dtype = n_q_heads, n_kv_heads, head_dim, dtype
+    d.n_pages, d.page_size, d.max_pages = n_pages, page_size, max_pages
+    d.rot_dim, d.eps, d.causal = head_dim if rot_dim is None else rot_dim, eps, int(causal)
+    d.softmax_scale = max(head_dim, 1) ** -0.5 if softmax_scale is None else softmax_scale
+    d.flags, d.table_stride = flags, max_pages if table_stride is None else table_stride
+    d.q_stride[:] = q_stride or (n_q_heads * head_dim, head_dim)
+    d.kv_stride[:] = kv_stride or (n_kv_heads * head_dim, head_dim)
+    d.o_stride[:] = o_stride or (n_q_heads * head_dim, head_dim)
+    d.cache_stride[:] = cache_stride or (n_kv_heads * page_size * head_dim, page_size * head_dim, head_dim)
+    return d
+
+
+def paged_append(desc: PagedDesc, q, k, v, q_weight, k_weight, inv_freq, positions, seq_start, kv_len, page_table, q_out, k_cache, v_cache,
+                 stream=None):
+    """loong_paged_append; weights and positions may be None, q and q_out together."""
+    t = desc.dtype
+    _check(lib.loong_paged_append(C.byref(desc), *_tensors(
+        ("q", q, t), ("k", k, t), ("v", v, t), ("q_weight", q_weight, FP32), ("k_weight", k_weight, FP32), ("inv_freq", inv_freq, FP32),
+        ("positions", positions, "i32"), ("seq_start", seq_start, "i32"), ("kv_len", kv_len, "i32"), ("page_table", page_table, "i32"),
+        ("q_out", q_out, t), ("k_cache", k_cache, t), ("v_cache", v_cache, t)), _stream(stream)))
+
+
+def paged_workspace_bytes(desc: PagedDesc) -> int:
+    """Bytes of caller-owned workspace paged_attn needs (0: none)."""
+    n = C.c_int64(0)
+    _check(lib.loong_paged_workspace_bytes(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def paged_attn(desc: PagedDesc, q, k_cache, v_cache, seq_start, kv_len, page_table, out, o, lse, workspace=None, workspace_bytes=None,
+               stream=None):
+    """loong_paged_attn; out (fp32) or o (the storage type) may be None; `workspace` as in attn_step_bwd."""
+    t = desc.dtype
+    _check(lib.loong_paged_attn(C.byref(desc), *_tensors(
+        ("q", q, t), ("k_cache", k_cache, t), ("v_cache", v_cache, t), ("seq_start", seq_start, "i32"), ("kv_len", kv_len, "i32"),
+        ("page_table", page_table, "i32"), ("out", out, FP32), ("o", o, t), ("lse", lse, FP32)),
+        *_workspace(workspace, workspace_bytes), _stream(stream)))

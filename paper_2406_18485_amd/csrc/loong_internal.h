@@ -123,4 +123,7 @@ int64_t bwd_steps_that_fit_bf16(const loong_step_desc& d, const StepGeom& g);
 // delta of every row, and with `head` the counters of a workspace cleared; these alone
 int launch_delta(const loong_step_desc& d, const void* o, const void* d_o, float* delta, void* head, void* stream);
 int launch_clear_head(void* head, void* stream);
+
+// Validate a descriptor of the paged cache (no device access); `flags`: those the call takes.
+int check_paged(const loong_paged_desc* d, int flags);
 }  // namespace loong
