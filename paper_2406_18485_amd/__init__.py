@@ -17,6 +17,9 @@ def __getattr__(name):
         return importlib.import_module(f"{__name__}.{name}")
     binding = importlib.import_module(f"{__name__}.binding")
     try:
-        return getattr(binding, name)
+        value = getattr(binding, name)
     except AttributeError:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}") from None
+    if callable(value):   # found once: this search is 4 to 10 us, as much as the rest of a call
+        globals()[name] = value
+    return value

@@ -150,36 +150,46 @@ def _ptr(x):
     return x.data_ptr()
 
 
-_torch_types = {}   # torch's of each dtype code
+_types = {}   # torch's type of each dtype code
+_device = None  # the current GPU's number
 
 
-def _tensors(*named):
-    """Device pointers of (name, tensor, dtype code or torch dtype), after the check that a kernel on the current device may
-    read them as what the call says they are; ints and None are passed through."""
-    ptrs, dev = [], None
-    for name, x, dtype in named:
-        if x is None or isinstance(x, int):
-            ptrs.append(x)
-            continue
-        if dev is None:
-            import torch
-            dev = torch.cuda.current_device() if torch.cuda.is_available() else -2
-            if not _torch_types:
-                _torch_types.update({BF16: torch.bfloat16, FP32: torch.float32, FP16: torch.float16, "i32": torch.int32})
-        if x.get_device() != dev:
-            raise ValueError(f"{name} is on {x.device}, not on the current GPU")
-        if x.dtype is not _torch_types.get(dtype, x.dtype):   # (an unknown code is the library's to refuse)
-            raise TypeError(f"{name} is {x.dtype}, not {_torch_types[dtype]}")
-        ptrs.append(x.data_ptr())
-    return ptrs
+def _find_device():
+    """Fills in `_types` and `_device` (a cheap query, as of the current stream; -2 without a GPU)."""
+    global _device
+    import torch
+    _types.update({BF16: torch.bfloat16, FP32: torch.float32, FP16: torch.float16, "i32": torch.int32})
+    if not torch.cuda.is_available():
+        _device = lambda: -2
+    else:
+        torch.cuda.current_device()  # initialises torch's side once
+        _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _workspace(x, n_bytes):
-    """(pointer, bytes) of a workspace tensor, or of a pointer with its size."""
-    (ptr,) = _tensors(("workspace", x, None))
-    if n_bytes is None:
-        n_bytes = 0 if x is None or isinstance(x, int) else x.numel() * x.element_size()
-    return ptr, n_bytes
+def _on(code):
+    """What _in compares a call's tensors with: the current GPU, torch's type of the dtype code (None: the library refuses it),
+    fp32 and int32."""
+    if _device is None:
+        _find_device()
+    return _device(), _types.get(code), _types[FP32], _types["i32"]
+
+
+def _in(x, dtype, dev, name):
+    """Device pointer of a tensor that a kernel on the current GPU may read as `dtype`; ints and None are passed through.
+    (A call has some ten: 0.3 us each, of a call's 6.)"""
+    if x is None or type(x) is int:
+        return x
+    if x.dtype is not dtype and dtype is not None:
+        raise TypeError(f"{name} is {x.dtype}, not {dtype}")
+    if x.get_device() != dev:
+        raise ValueError(f"{name} is on {x.device}, not on the current GPU")
+    return x.data_ptr()
+
+
+def _workspace_bytes(x, n_bytes):
+    if n_bytes is not None:
+        return n_bytes
+    return 0 if x is None or type(x) is int else x.numel() * x.element_size()
 
 
 def pointer_array(addresses):
@@ -394,10 +404,11 @@ def make_rope_desc(*, batch, n_q_heads, n_kv_heads, head_dim, len, dtype, rot_di
 
 def qk_rope_fwd(desc: RopeDesc, q, k, q_weight, k_weight, inv_freq, positions, q_out, k_out, stream=None):
     """loong_qk_rope_fwd; weights, positions (and what of q, k is not there) may be None."""
-    t = desc.dtype
-    _check(lib.loong_qk_rope_fwd(C.byref(desc), *_tensors(
-        ("q", q, t), ("k", k, t), ("q_weight", q_weight, FP32), ("k_weight", k_weight, FP32), ("inv_freq", inv_freq, FP32),
-        ("positions", positions, "i32"), ("q_out", q_out, t), ("k_out", k_out, t)), _stream(stream)))
+    dev, t, f32, i32 = _on(desc.dtype)
+    _check(lib.loong_qk_rope_fwd(
+        C.byref(desc), _in(q, t, dev, "q"), _in(k, t, dev, "k"), _in(q_weight, f32, dev, "q_weight"), _in(k_weight, f32, dev, "k_weight"),
+        _in(inv_freq, f32, dev, "inv_freq"), _in(positions, i32, dev, "positions"), _in(q_out, t, dev, "q_out"), _in(k_out, t, dev, "k_out"),
+        _stream(stream)))
 
 
 def qk_rope_workspace_bytes(desc: RopeDesc) -> int:
@@ -409,11 +420,13 @@ def qk_rope_workspace_bytes(desc: RopeDesc) -> int:
 def qk_rope_bwd(desc: RopeDesc, q, k, q_weight, k_weight, inv_freq, positions, d_q_out, d_k_out, dq, dk, dq_weight=None, dk_weight=None,
                 workspace=None, workspace_bytes=None, stream=None):
     """loong_qk_rope_bwd; `workspace` as in attn_step_bwd."""
-    t = desc.dtype
-    _check(lib.loong_qk_rope_bwd(C.byref(desc), *_tensors(
-        ("q", q, t), ("k", k, t), ("q_weight", q_weight, FP32), ("k_weight", k_weight, FP32), ("inv_freq", inv_freq, FP32),
-        ("positions", positions, "i32"), ("d_q_out", d_q_out, FP32), ("d_k_out", d_k_out, FP32), ("dq", dq, t), ("dk", dk, t),
-        ("dq_weight", dq_weight, FP32), ("dk_weight", dk_weight, FP32)), *_workspace(workspace, workspace_bytes), _stream(stream)))
+    dev, t, f32, i32 = _on(desc.dtype)
+    _check(lib.loong_qk_rope_bwd(
+        C.byref(desc), _in(q, t, dev, "q"), _in(k, t, dev, "k"), _in(q_weight, f32, dev, "q_weight"), _in(k_weight, f32, dev, "k_weight"),
+        _in(inv_freq, f32, dev, "inv_freq"), _in(positions, i32, dev, "positions"), _in(d_q_out, f32, dev, "d_q_out"),
+        _in(d_k_out, f32, dev, "d_k_out"), _in(dq, t, dev, "dq"), _in(dk, t, dev, "dk"), _in(dq_weight, f32, dev, "dq_weight"),
+        _in(dk_weight, f32, dev, "dk_weight"), _in(workspace, None, dev, "workspace"), _workspace_bytes(workspace, workspace_bytes),
+        _stream(stream)))
 
 
 def make_paged_desc(*, n_seqs, n_tokens, n_q_heads, n_kv_heads, head_dim, dtype, n_pages, page_size, max_pages, max_new=None, rot_dim=None,
@@ -438,11 +451,12 @@ def make_paged_desc(*, n_seqs, n_tokens, n_q_heads, n_kv_heads, head_dim, dtype,
 def paged_append(desc: PagedDesc, q, k, v, q_weight, k_weight, inv_freq, positions, seq_start, kv_len, page_table, q_out, k_cache, v_cache,
                  stream=None):
     """loong_paged_append; weights and positions may be None, q and q_out together."""
-    t = desc.dtype
-    _check(lib.loong_paged_append(C.byref(desc), *_tensors(
-        ("q", q, t), ("k", k, t), ("v", v, t), ("q_weight", q_weight, FP32), ("k_weight", k_weight, FP32), ("inv_freq", inv_freq, FP32),
-        ("positions", positions, "i32"), ("seq_start", seq_start, "i32"), ("kv_len", kv_len, "i32"), ("page_table", page_table, "i32"),
-        ("q_out", q_out, t), ("k_cache", k_cache, t), ("v_cache", v_cache, t)), _stream(stream)))
+    dev, t, f32, i32 = _on(desc.dtype)
+    _check(lib.loong_paged_append(
+        C.byref(desc), _in(q, t, dev, "q"), _in(k, t, dev, "k"), _in(v, t, dev, "v"), _in(q_weight, f32, dev, "q_weight"),
+        _in(k_weight, f32, dev, "k_weight"), _in(inv_freq, f32, dev, "inv_freq"), _in(positions, i32, dev, "positions"),
+        _in(seq_start, i32, dev, "seq_start"), _in(kv_len, i32, dev, "kv_len"), _in(page_table, i32, dev, "page_table"),
+        _in(q_out, t, dev, "q_out"), _in(k_cache, t, dev, "k_cache"), _in(v_cache, t, dev, "v_cache"), _stream(stream)))
 
 
 def paged_workspace_bytes(desc: PagedDesc) -> int:
@@ -455,8 +469,9 @@ def paged_workspace_bytes(desc: PagedDesc) -> int:
 def paged_attn(desc: PagedDesc, q, k_cache, v_cache, seq_start, kv_len, page_table, out, o, lse, workspace=None, workspace_bytes=None,
                stream=None):
     """loong_paged_attn; out (fp32) or o (the storage type) may be None; `workspace` as in attn_step_bwd."""
-    t = desc.dtype
-    _check(lib.loong_paged_attn(C.byref(desc), *_tensors(
-        ("q", q, t), ("k_cache", k_cache, t), ("v_cache", v_cache, t), ("seq_start", seq_start, "i32"), ("kv_len", kv_len, "i32"),
-        ("page_table", page_table, "i32"), ("out", out, FP32), ("o", o, t), ("lse", lse, FP32)),
-        *_workspace(workspace, workspace_bytes), _stream(stream)))
+    dev, t, f32, i32 = _on(desc.dtype)
+    _check(lib.loong_paged_attn(
+        C.byref(desc), _in(q, t, dev, "q"), _in(k_cache, t, dev, "k_cache"), _in(v_cache, t, dev, "v_cache"),
+        _in(seq_start, i32, dev, "seq_start"), _in(kv_len, i32, dev, "kv_len"), _in(page_table, i32, dev, "page_table"),
+        _in(out, f32, dev, "out"), _in(o, t, dev, "o"), _in(lse, f32, dev, "lse"), _in(workspace, None, dev, "workspace"),
+        _workspace_bytes(workspace, workspace_bytes), _stream(stream)))

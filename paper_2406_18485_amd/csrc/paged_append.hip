@@ -128,9 +128,9 @@ int loong_paged_append(const loong_paged_desc* desc, const void* q, const void* 
   if (norm && !(std::isfinite(d.eps) && d.eps >= 0.f)) return fail(LOONG_E_SHAPE, "eps must be finite and not negative");
   if (!k || !v || !seq_start || !kv_len || !page_table || !k_cache || !v_cache || (d.rot_dim > 0 && !inv_freq) || !q != !q_out)
     return fail(LOONG_E_NULL, "loong_paged_append: NULL argument");
-  for (const void* x : {q, k, v, (const void*)q_weight, (const void*)k_weight, (const void*)q_out, (const void*)k_cache, (const void*)v_cache})
+  for (const void* x : {q, k, v, (const void*)q_weight, (const void*)k_weight, (const void*)inv_freq, (const void*)q_out, (const void*)k_cache, (const void*)v_cache})
     if (!aligned16(x)) return fail(LOONG_E_ALIGN, "loong_paged_append: tensor not 16-byte aligned");
-  for (const void* x : {(const void*)inv_freq, (const void*)positions, (const void*)seq_start, (const void*)kv_len, (const void*)page_table})
+  for (const void* x : {(const void*)positions, (const void*)seq_start, (const void*)kv_len, (const void*)page_table})
     if (reinterpret_cast<uintptr_t>(x) & 3) return fail(LOONG_E_ALIGN, "loong_paged_append: table or inv_freq not 4-byte aligned");
   if (d.n_tokens == 0 || d.n_seqs == 0) return LOONG_OK;
   AppendParams p{};

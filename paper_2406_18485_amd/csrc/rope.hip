@@ -28,7 +28,8 @@ struct RopeParams {
   int32_t heads[2];
   int32_t heads_per_group;       // heads that a group of lanes walks over
   int64_t token_blocks;
-  float* partial;                // backward: sums over a workgroup's rows, [workgroup][q, k][head_dim], or NULL
+  int32_t bwd_heads[2], bwd_blocks[2], bwd_wgs_q;   // backward: heads and workgroups of a share; the first so many workgroups are q's
+  float* partial;                // backward: sums over a workgroup's rows, [workgroup][head_dim], or NULL
   int32_t head_dim;
 };
 
@@ -48,15 +49,15 @@ __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeParams
   if (token >= p.tokens) return;
   const int b = (int)(token / p.len), t = (int)(token - (int64_t)b * p.len);
   RopeLane<E, INTER> lane(p.row, s);
-  lane.turn(p.row, s, position_of(p, token, b, t));
+  const int64_t pos = position_of(p, token, b, t);
   const int h_lo = blockIdx.y * p.heads_per_group, h_hi = min(h_lo + p.heads_per_group, p.heads[0] + p.heads[1]);
+  bool turned = false;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     const int from = which ? p.heads[0] : 0;
     const int lo = max(h_lo, from) - from, hi = min(h_hi, from + p.heads[which]) - from;
     if (lo >= hi) continue;
     float w[2 * V];
-    if (p.row.norm) lane.weights(p.w[which], w);
     const T* x = (const T*)p.x[which] + b * p.xs[which][0] + t * p.xs[which][2];
     T* y = (T*)p.y[which] + b * p.ys[which][0] + t * p.ys[which][2];
     for (int h = lo; h < hi; h += AT_ONCE) {
@@ -67,14 +68,17 @@ __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeParams
         pa[j] = *reinterpret_cast<const uint4*>(row + lane.a);
         pb[j] = *reinterpret_cast<const uint4*>(row + lane.b);
       }
+      if (h == lo && p.row.norm) lane.weights(p.w[which], w);
+      if (!turned) lane.turn(p.row, s, pos);   // (while the first rows are on their way)
+      turned = true;
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j) {
         if (h + j >= hi) break;
         lane.forward(p.row, w, pa[j], pb[j]);
         T* row = y + (int64_t)(h + j) * p.ys[which][1];
         if (lane.holds) {
-          *reinterpret_cast<uint4*>(row + lane.a) = pa[j];
-          *reinterpret_cast<uint4*>(row + lane.b) = pb[j];
+          store_streaming(row + lane.a, pa[j]);
+          store_streaming(row + lane.b, pb[j]);
         }
       }
     }
@@ -82,7 +86,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeParams
 }
 
 // dx = r (w g) - x r^3 mean(w g x), g the gradient rotated back; a weight's gradient is the sum of g x r over all rows.
-// A workgroup walks over token blocks; its sums go to the workspace, and the kernel behind this one adds them up in order.
+// A workgroup takes heads of q or of k and walks over token blocks, the next row's loads in flight while one is computed; its
+// sums go to the workspace, and the kernel behind this one adds them up in order.
 template <class E, bool INTER>
 __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeParams p) {
   typedef typename StorageOf<E>::type T;
@@ -90,101 +95,129 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeParams
   __shared__ float sums[kRopeThreads / 64][64][2 * V];
   const int lanes = 1 << p.row.lg, s = threadIdx.x & (lanes - 1);
   RopeLane<E, INTER> lane(p.row, s);
-  const int h_lo = blockIdx.y * p.heads_per_group, h_hi = min(h_lo + p.heads_per_group, p.heads[0] + p.heads[1]);
-  float dw[2][2 * V];
+  const int which = (int)blockIdx.x >= p.bwd_wgs_q, wg = blockIdx.x - (which ? p.bwd_wgs_q : 0), blocks = p.bwd_blocks[which];
+  const int share = wg / blocks, lo = share * p.bwd_heads[which], hi = min(lo + p.bwd_heads[which], p.heads[which]);
+  const int64_t* const xs = p.xs[which];
+  const int64_t* const ys = p.ys[which];
+  float w[2 * V], dw[2 * V];
+  if (p.row.norm) lane.weights(p.w[which], w);
 #pragma unroll
-  for (int which = 0; which < 2; ++which)
-#pragma unroll
-    for (int i = 0; i < 2 * V; ++i) dw[which][i] = 0.f;
-  for (int64_t block = blockIdx.x; block < p.token_blocks; block += gridDim.x) {
-    const int64_t token = block * (kRopeThreads >> p.row.lg) + (threadIdx.x >> p.row.lg);
-    if (token >= p.tokens) break;   // (only in the last block)
+  for (int i = 0; i < 2 * V; ++i) dw[i] = 0.f;
+  // one row of a token: where it is, and what is loaded of it
+  struct Row {
+    int64_t x, g;
+    uint4 xa, xb;
+    float4 v[V / 2];
+  };
+  const int per = kRopeThreads >> p.row.lg, group = threadIdx.x >> p.row.lg;
+  int64_t block = wg - share * blocks, token = block * per + group;
+  int h = lo;
+  auto load = [&](int64_t token, int h) {
     const int b = (int)(token / p.len), t = (int)(token - (int64_t)b * p.len);
-    lane.turn(p.row, s, position_of(p, token, b, t));
+    Row r;
+    r.x = b * xs[0] + h * xs[1] + t * xs[2];
+    r.g = b * ys[0] + h * ys[1] + t * ys[2];
+    const float* grow = p.g[which] + r.g;
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      const int from = which ? p.heads[0] : 0;
-      const int lo = max(h_lo, from) - from, hi = min(h_hi, from + p.heads[which]) - from;
-      if (lo >= hi) continue;
-      float w[2 * V];
-      if (p.row.norm) lane.weights(p.w[which], w);
-      const T* x = (const T*)p.x[which] + b * p.xs[which][0] + t * p.xs[which][2];
-      const float* g = p.g[which] + b * p.ys[which][0] + t * p.ys[which][2];
-      T* dx = (T*)p.y[which] + b * p.xs[which][0] + t * p.xs[which][2];
-      for (int h = lo; h < hi; ++h) {
-        float gy[2 * V];
-        const float* grow = g + (int64_t)h * p.ys[which][1];
+    for (int i = 0; i < 2 * V; i += 4) r.v[i / 4] = *reinterpret_cast<const float4*>(grow + (i < V ? lane.a + i : lane.b + i - V));
+    if (p.row.norm) {
+      const T* row = (const T*)p.x[which] + r.x;
+      r.xa = *reinterpret_cast<const uint4*>(row + lane.a);
+      r.xb = *reinterpret_cast<const uint4*>(row + lane.b);
+    }
+    return r;
+  };
+  Row next;
+  if (token < p.tokens) next = load(token, h);
+  while (token < p.tokens) {   // (past it in a last block of few tokens, and then in every later one)
+    const Row cur = next;
+    if (h == lo) {
+      const int b = (int)(token / p.len);
+      lane.turn(p.row, s, position_of(p, token, b, (int)(token - (int64_t)b * p.len)));
+    }
+    if (++h == hi) {
+      h = lo;
+      block += blocks;
+      token = block * per + group;
+    }
+    if (token < p.tokens) next = load(token, h);
+    float gy[2 * V];
 #pragma unroll
-        for (int i = 0; i < 2 * V; i += 4) {
-          const float4 v4 = *reinterpret_cast<const float4*>(grow + (i < V ? lane.a + i : lane.b + i - V));
-          gy[i] = v4.x; gy[i + 1] = v4.y; gy[i + 2] = v4.z; gy[i + 3] = v4.w;
-        }
-        lane.rotate_back(gy);
-        if (p.row.norm) {
-          float xv[2 * V];
-          const T* row = x + (int64_t)h * p.xs[which][1];
-          unpack16<E>(*reinterpret_cast<const uint4*>(row + lane.a), xv);
-          unpack16<E>(*reinterpret_cast<const uint4*>(row + lane.b), xv + V);
-          const float inv = lane.rms(p.row, xv);
-          float dot = 0.f;
+    for (int i = 0; i < 2 * V; i += 4) {
+      gy[i] = cur.v[i / 4].x; gy[i + 1] = cur.v[i / 4].y; gy[i + 2] = cur.v[i / 4].z; gy[i + 3] = cur.v[i / 4].w;
+    }
+    lane.rotate_back(gy);
+    if (p.row.norm) {
+      float xv[2 * V];
+      unpack16<E>(cur.xa, xv);
+      unpack16<E>(cur.xb, xv + V);
+      // both sums of the row at once
+      float sq = 0.f, dot = 0.f;
 #pragma unroll
-          for (int i = 0; i < 2 * V; ++i) {
-            dw[which][i] += gy[i] * (xv[i] * inv);
-            gy[i] *= w[i];
-            dot += gy[i] * xv[i];
-          }
-          const float c = lane.row_sum(p.row, dot) * p.row.inv_d * (inv * inv * inv);
-#pragma unroll
-          for (int i = 0; i < 2 * V; ++i) gy[i] = gy[i] * inv - xv[i] * c;
-        }
-        T* row = dx + (int64_t)h * p.xs[which][1];
-        if (lane.holds) {
-          *reinterpret_cast<uint4*>(row + lane.a) = pack16<E>(gy);
-          *reinterpret_cast<uint4*>(row + lane.b) = pack16<E>(gy + V);
-        }
+      for (int i = 0; i < 2 * V; ++i) {
+        sq += xv[i] * xv[i];
+        dot += gy[i] * w[i] * xv[i];
       }
+      lane.row_sums(p.row, sq, dot);
+      const float inv = rsqrtf(sq * p.row.inv_d + p.row.eps), c = dot * p.row.inv_d * (inv * inv * inv);
+#pragma unroll
+      for (int i = 0; i < 2 * V; ++i) {
+        dw[i] += gy[i] * (xv[i] * inv);
+        gy[i] = gy[i] * w[i] * inv - xv[i] * c;
+      }
+    }
+    T* row = (T*)p.y[which] + cur.x;
+    if (lane.holds) {
+      store_streaming(row + lane.a, pack16<E>(gy));
+      store_streaming(row + lane.b, pack16<E>(gy + V));
     }
   }
   if (!p.partial) return;
   // sums over the workgroup's groups: across a wave by exchange, across the waves through LDS, in a fixed order
   const int wave = threadIdx.x >> 6, l = threadIdx.x & 63;
-  float* mine = p.partial + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * p.head_dim;
+  float* mine = p.partial + (int64_t)blockIdx.x * p.head_dim;
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
+  for (int i = 0; i < 2 * V; ++i) {
+    float x = dw[i];
+    for (int m = 32; m >= lanes; m >>= 1) x += __shfl_xor(x, m, 64);
+    if (l < lanes) sums[wave][l][i] = x;
+  }
+  __syncthreads();
+  if (threadIdx.x < lanes && lane.holds) {
 #pragma unroll
     for (int i = 0; i < 2 * V; ++i) {
-      float x = dw[which][i];
-      for (int m = 32; m >= lanes; m >>= 1) x += __shfl_xor(x, m, 64);
-      if (l < lanes) sums[wave][l][i] = x;
-    }
-    __syncthreads();
-    if (threadIdx.x < lanes && lane.holds) {
+      float x = 0.f;
 #pragma unroll
-      for (int i = 0; i < 2 * V; ++i) {
-        float x = 0.f;
-#pragma unroll
-        for (int k = 0; k < kRopeThreads / 64; ++k) x += sums[k][s][i];
-        mine[which * p.head_dim + (i < V ? lane.a + i : lane.b + i - V)] = x;
-      }
+      for (int k = 0; k < kRopeThreads / 64; ++k) x += sums[k][s][i];
+      mine[i < V ? lane.a + i : lane.b + i - V] = x;
     }
-    __syncthreads();
   }
 }
 
-// The workgroups' sums, added up: 16 columns a workgroup, 16 threads a column, each over every 16th of them.
-__global__ __launch_bounds__(256) void rope_weight_kernel(const float* partial, int n, int head_dim, float* dwq, float* dwk) {
-  __shared__ float sums[16][17];
-  const int c = threadIdx.x & 15, part = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+// The workgroups' sums (those of q first), added up: 16 columns a workgroup, 64 threads a column.  Bound by the chain of loads:
+// one in 64 of them each, eight at a time.  (16 threads a column: 14 us for 1024 sums.)
+constexpr int kWeightThreads = 1024;
+__global__ __launch_bounds__(kWeightThreads) void rope_weight_kernel(const float* partial, int nq, int nk, int head_dim, float* dwq, float* dwk) {
+  __shared__ float sums[64][17];
+  const int c = threadIdx.x & 15, part = threadIdx.x >> 4, at = blockIdx.x * 16 + c;
+  const int which = at >= head_dim, col = at - which * head_dim, n = which ? nk : nq;
+  const float* from = partial + (int64_t)(which ? nq : 0) * head_dim + col;
   float x = 0.f;
-  for (int i = part; i < n; i += 16) x += partial[(int64_t)i * 2 * head_dim + col];
+  for (int i = part; i < n; i += 64 * 8) {
+    float y[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = i + 64 * k < n ? from[(int64_t)(i + 64 * k) * head_dim] : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x += y[k];
+  }
   sums[part][c] = x;
   __syncthreads();
   if (part) return;
   x = 0.f;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) x += sums[k][c];
-  float* dw = col < head_dim ? dwq : dwk;
-  if (dw) dw[col < head_dim ? col : col - head_dim] = x;
+  for (int k = 0; k < 64; ++k) x += sums[k][c];
+  float* dw = which ? dwk : dwq;
+  if (dw) dw[col] = x;
 }
 
 int check_rope(const loong_rope_desc* d) {
@@ -217,23 +250,33 @@ int check_rope(const loong_rope_desc* d) {
   return LOONG_OK;
 }
 
-// Token blocks x shares of the heads.  A group of lanes takes so many heads that the launch still has some 16 waves for
-// every unit; the backward's token blocks are walked over by at most four workgroups a unit, so that few sums are left.
+// Forward: token blocks x shares of the heads; a group of lanes takes so many heads that the launch still has some `kFwdPerCu`
+// workgroups for every unit.  Backward: a workgroup has heads of q or of k and walks over every so-manieth token block; there are as
+// many of either as gives all of them equal work and every unit about `kBwdPerCu`, what its registers have room for.
+constexpr int kFwdPerCu = 4, kBwdPerCu = 3;
 struct RopePlan {
   int64_t token_blocks;
   int heads_per_group, shares;
-  int64_t bwd_blocks;     // workgroups of a share
+  struct { int heads_per_group, shares; int64_t blocks; } bwd[2];   // q, k: `blocks` workgroups a share
+  int64_t bwd_workgroups(int which) const { return bwd[which].shares * bwd[which].blocks; }
 };
 RopePlan plan_rope(const loong_rope_desc& d, const RopeRow& r, int cus) {
   RopePlan p{};
   const int64_t tokens = (int64_t)d.batch * d.len, per = kRopeThreads >> r.lg;
-  const int heads = d.n_q_heads + d.n_kv_heads;
+  const int heads[3] = {d.n_q_heads, d.n_kv_heads, d.n_q_heads + d.n_kv_heads};
   p.token_blocks = (tokens + per - 1) / per;
-  const int64_t hpg = p.token_blocks * heads / (4 * (int64_t)cus);
-  p.heads_per_group = hpg < 1 ? 1 : hpg > heads ? heads : (int)hpg;
-  p.shares = (heads + p.heads_per_group - 1) / p.heads_per_group;
-  const int64_t most = (4 * (int64_t)cus + p.shares - 1) / p.shares;
-  p.bwd_blocks = p.token_blocks < most ? p.token_blocks : most;
+  const int64_t rows = p.token_blocks * heads[2];   // of lane groups: rows that a workgroup handles at a time
+  const int64_t hpg = (rows + kFwdPerCu * (int64_t)cus - 1) / (kFwdPerCu * (int64_t)cus);
+  p.heads_per_group = hpg < 1 ? 1 : hpg > heads[2] ? heads[2] : (int)hpg;
+  p.shares = (heads[2] + p.heads_per_group - 1) / p.heads_per_group;
+  const int64_t each = (rows + kBwdPerCu * (int64_t)cus - 1) / (kBwdPerCu * (int64_t)cus);   // rows a workgroup
+  for (int k = 0; k < 2; ++k) {
+    if (heads[k] == 0 || rows == 0) continue;
+    p.bwd[k].heads_per_group = each > heads[k] ? heads[k] : (int)each;
+    p.bwd[k].shares = (heads[k] + p.bwd[k].heads_per_group - 1) / p.bwd[k].heads_per_group;
+    const int64_t blocks_each = (each + p.bwd[k].heads_per_group - 1) / p.bwd[k].heads_per_group;
+    p.bwd[k].blocks = (p.token_blocks + blocks_each - 1) / blocks_each;
+  }
   return p;
 }
 
@@ -244,7 +287,7 @@ RopeRow row_of(const loong_rope_desc& d, const float* inv_freq) {
 int64_t rope_workspace(const loong_rope_desc& d, int cus) {
   if (!(d.flags & LOONG_QK_NORM)) return 0;
   const RopePlan pl = plan_rope(d, row_of(d, nullptr), cus);
-  return pl.bwd_blocks * pl.shares * 2 * d.head_dim * 4;
+  return (pl.bwd_workgroups(0) + pl.bwd_workgroups(1)) * d.head_dim * 4;
 }
 
 // what both calls ask of their tensors; `names` of q and of its other tensors
@@ -255,8 +298,8 @@ int check_rope_tensors(const loong_rope_desc& d, const char* what, const float* 
     if ((d.n_q_heads > 0 && !q[i]) || (d.n_kv_heads > 0 && !k[i])) return fail(LOONG_E_NULL, "%s: NULL tensor", what);
     if ((d.n_q_heads > 0 && !aligned16(q[i])) || (d.n_kv_heads > 0 && !aligned16(k[i]))) return fail(LOONG_E_ALIGN, "%s: tensor not 16-byte aligned", what);
   }
-  if (!aligned16(w[0]) || !aligned16(w[1])) return fail(LOONG_E_ALIGN, "%s: weights not 16-byte aligned", what);
-  if ((reinterpret_cast<uintptr_t>(inv_freq) | reinterpret_cast<uintptr_t>(positions)) & 3) return fail(LOONG_E_ALIGN, "%s: inv_freq or positions not 4-byte aligned", what);
+  if (!aligned16(w[0]) || !aligned16(w[1]) || !aligned16(inv_freq)) return fail(LOONG_E_ALIGN, "%s: weights or inv_freq not 16-byte aligned", what);
+  if ((reinterpret_cast<uintptr_t>(positions)) & 3) return fail(LOONG_E_ALIGN, "%s: positions not 4-byte aligned", what);
   return LOONG_OK;
 }
 
@@ -271,7 +314,7 @@ RopeParams params_of(const loong_rope_desc& d, const RopePlan& pl, const float* 
   p.tokens = (int64_t)d.batch * d.len;
   p.len = d.len; p.chunk_len = d.chunk_len; p.chunk[0] = d.chunk[0]; p.chunk[1] = d.chunk[1];
   p.heads[0] = d.n_q_heads; p.heads[1] = d.n_kv_heads;
-  p.heads_per_group = pl.heads_per_group; p.token_blocks = pl.token_blocks; p.head_dim = d.head_dim;
+  p.token_blocks = pl.token_blocks; p.head_dim = d.head_dim;
   return p;
 }
 
@@ -304,6 +347,7 @@ int loong_qk_rope_fwd(const loong_rope_desc* desc, const void* q, const void* k,
   if (pl.token_blocks == 0) return LOONG_OK;
   if (pl.shares > 65535 || !launch_fits(pl.token_blocks * pl.shares, kRopeThreads)) return fail(LOONG_E_UNSUPPORTED, "loong_qk_rope_fwd: grid too large");
   RopeParams p = params_of(*desc, pl, inv_freq, positions);
+  p.heads_per_group = pl.heads_per_group;
   p.x[0] = q; p.x[1] = k; p.w[0] = q_weight; p.w[1] = k_weight; p.y[0] = q_out; p.y[1] = k_out;
   const dim3 grid((unsigned)pl.token_blocks, (unsigned)pl.shares);
   const bool inter = (desc->flags & LOONG_ROPE_INTERLEAVED) != 0;
@@ -344,13 +388,16 @@ int loong_qk_rope_bwd(const loong_rope_desc* desc, const void* q, const void* k,
     if (workspace_bytes < need)
       return fail(LOONG_E_SHAPE, "loong_qk_rope_bwd: workspace of %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
   }
-  if (pl.shares > 65535 || !launch_fits(pl.bwd_blocks * pl.shares, kRopeThreads)) return fail(LOONG_E_UNSUPPORTED, "loong_qk_rope_bwd: grid too large");
+  const int64_t nq = pl.bwd_workgroups(0), nk = pl.bwd_workgroups(1);
+  if (!launch_fits(nq + nk, kRopeThreads)) return fail(LOONG_E_UNSUPPORTED, "loong_qk_rope_bwd: grid too large");
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (pl.token_blocks > 0) {
     RopeParams p = params_of(*desc, pl, inv_freq, positions);
+    for (int i = 0; i < 2; ++i) { p.bwd_heads[i] = pl.bwd[i].heads_per_group; p.bwd_blocks[i] = (int)pl.bwd[i].blocks; }
+    p.bwd_wgs_q = (int)nq;
     p.x[0] = q; p.x[1] = k; p.w[0] = q_weight; p.w[1] = k_weight; p.y[0] = dq; p.y[1] = dk; p.g[0] = d_q_out; p.g[1] = d_k_out;
     p.partial = sums ? static_cast<float*>(workspace) : nullptr;
-    const dim3 grid((unsigned)pl.bwd_blocks, (unsigned)pl.shares);
+    const dim3 grid((unsigned)(nq + nk));
     const bool inter = (desc->flags & LOONG_ROPE_INTERLEAVED) != 0;
     if (desc->dtype == LOONG_BF16) launch_rope_bwd<Bf16>(p, grid, inter, st);
     else if (desc->dtype == LOONG_FP16) launch_rope_bwd<Fp16>(p, grid, inter, st);
@@ -358,8 +405,8 @@ int loong_qk_rope_bwd(const loong_rope_desc* desc, const void* q, const void* k,
     if (int rc = check_launch("loong_qk_rope_bwd")) return rc;
   }
   if (!sums) return LOONG_OK;
-  rope_weight_kernel<<<dim3((unsigned)(2 * desc->head_dim / 16)), dim3(256), 0, st>>>(
-      static_cast<const float*>(workspace), (int)(pl.bwd_blocks * pl.shares), desc->head_dim, dq_weight, dk_weight);
+  rope_weight_kernel<<<dim3((unsigned)(2 * desc->head_dim / 16)), dim3(kWeightThreads), 0, st>>>(
+      static_cast<const float*>(workspace), (int)nq, (int)nk, desc->head_dim, dq_weight, dk_weight);
   return check_launch("loong_qk_rope_bwd (weights)");
 }
 
