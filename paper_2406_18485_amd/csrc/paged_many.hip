@@ -1,0 +1,374 @@
+// Paged attention of many rows (a chunk of a prompt, alone or beside decoding sequences).
+//
+// Bound by the matrix cores and what feeds them, like the forward step (attn_fwd.hip), whose loop this is: eight waves = 8 / KS blocks
+// of 32 rows x KS key splits; a tile of K and V is staged for all of them, several tiles deep.  The query rows of a kv head (token by
+// token, the group's q heads of each) are cut into tiles of 256 / KS; KS is the smallest that gives every unit of the chip a tile (fewer
+// rows a workgroup read the same keys more often, but are more workgroups without an exchange between them).
+//
+// Division.  A unit (sequence, kv head, row tile) is cut into spans of keys where that shortens the launch.  The lengths are in
+// device memory: every wave works out, for a few lengths of a span, how many spans there would be and about how long they would
+// take, and all take the best one.  A cut unit's spans are added up by the last to arrive (split_exchange.h), kManyFan at a time.
+#include <hip/hip_runtime.h>
+
+#include "paged_body.h"
+
+namespace loong {
+namespace {
+
+constexpr int kManyWaves = 8;
+constexpr int kManyFan = 4;            // parts that are added up at a time
+constexpr int kManyLevels = 6;         // 4^6 parts are more than a unit has
+constexpr int kManyLeast = 256;        // keys of a span of a cut unit, at the least
+constexpr int kManyFixed = 512;        // what a span costs besides its keys, in keys
+constexpr int kManyMore = 2;           // spans that cutting may add, per unit of the chip
+
+struct ManySpan {
+  Unit u;
+  int keys, part;
+  int slot;                // number of the unit's first span among those of all cut units
+};
+
+// Every wave for itself: a lane looks at sequences lane, lane + 64, ...
+template <int ROWS>
+__device__ __forceinline__ bool find_span(const PagedParams& p, int cus, ManySpan& out) {
+  const int lane = threadIdx.x & 63;
+  auto tiles_of = [&](const Seq& s) { return (s.rows + ROWS - 1) / ROWS; };
+  auto parts_of = [](const Seq& s, int keys) { return s.paged <= keys ? 1 : (int)((uint32_t)(s.paged - 1) / (uint32_t)keys) + 1; };
+  Seq mine{};
+  if (lane < p.n_seqs) mine = sequence(p, lane);
+  auto seq_at = [&](int base) {
+    Seq s = mine;
+    if (base > 0) {
+      s = Seq{};
+      if (base + lane < p.n_seqs) s = sequence(p, base + lane);
+    }
+    return s;
+  };
+  float load = 0.f, units = 0.f;
+  int most = 0;
+  for (int base = 0; base < p.n_seqs; base += 64) {
+    const Seq s = seq_at(base);
+    const int t = tiles_of(s);
+    load += (float)t * (float)s.paged;
+    units += (float)t;
+    most = max(most, t ? s.paged : 0);
+  }
+  load = wave_total(load) * p.hkv;
+  units = wave_total(units) * p.hkv;
+  most = wave_most(most);
+  if (units == 0.f || units > (float)gridDim.x) return false;   // (more than there can be: seq_start decreases somewhere)
+  // the span that ends first: all alike, in rounds; unequal, in what is left of a unit of the chip after equal work
+  const float per_cu = load / cus;
+  const int fit = (int)(cus / units);   // parts that give every unit of the chip one
+  int keys = 0, all = 0;
+  float best = INFINITY;
+#pragma unroll 1
+  for (int c = 0; c < 6; ++c) {
+    const int cut = c < 4 ? (c + 1) * max(fit, 1) : 1;
+    int k = c < 4 ? (int)(((int64_t)most + cut - 1) / cut) : c == 4 ? (int)fminf(per_cu, 2e9f) : (int)fminf(0.5f * per_cu, 2e9f);
+    k = max(k < 0x7fffff00 ? (k + 63) / 64 * 64 : k, kManyLeast);
+    // (what bounds the number of spans, and their slots: cutting adds at most kManyMore a unit of the chip)
+    if (load > (float)k * (float)(kManyMore * cus) * 0.999f && k < most) continue;
+    int n = 0;
+    for (int base = 0; base < p.n_seqs; base += 64) {
+      const Seq s = seq_at(base);
+      n += tiles_of(s) * parts_of(s, k);
+    }
+    n = wave_total(n) * p.hkv;
+    const float cost = k >= most ? (float)most : (float)k;
+    const float rounds = (float)((n + cus - 1) / cus), est = 0.5f * (rounds * (cost + kManyFixed) + per_cu + (float)n / cus * kManyFixed);
+    if (est < best) { best = est; keys = k; all = n; }
+  }
+  if (keys == 0 || all > (int)gridDim.x) return false;   // (never: not to cut at all is always among them)
+  // neighbours share an XCD and its L2 where they read the same keys
+  const int per = (all + 7) / 8, idx = blockIdx.x >> 3, item = (int)(blockIdx.x & 7) * per + idx;
+  if (idx >= per || item >= all) return false;
+  int before = 0, slot = 0;
+  for (int base = 0; base < p.n_seqs; base += 64) {
+    const Seq s = seq_at(base);
+    const int parts = parts_of(s, keys), n = tiles_of(s) * parts * p.hkv, cut = parts > 1 ? n : 0;
+    const int upto = wave_prefix(n), slots = wave_prefix(cut);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > item);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      const int at = item - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
+      out.u.b = base + l;
+      out.u.start = __builtin_amdgcn_readlane(s.start, l); out.u.n = __builtin_amdgcn_readlane(s.n, l);
+      out.u.rows = __builtin_amdgcn_readlane(s.rows, l); out.u.kv = __builtin_amdgcn_readlane(s.kv, l);
+      const int np = __builtin_amdgcn_readlane(parts, l), nt = (out.u.rows + ROWS - 1) / ROWS;
+      out.keys = keys;
+      out.u.hk = at / (np * nt);
+      const int rest = at - out.u.hk * np * nt;
+      out.part = rest / nt;
+      out.u.tile = nt - 1 - (rest - out.part * nt);      // (the tiles that see most first)
+      out.slot = slot + __builtin_amdgcn_readlane(slots, l) - __builtin_amdgcn_readlane(cut, l) + (out.u.hk * nt + out.u.tile) * np;
+      return true;
+    }
+    before += last_lane(upto);
+    slot += last_lane(slots);
+  }
+  return false;
+}
+
+template <int D, int KS>
+struct ManyCfg {
+  static constexpr int NRB = kManyWaves / KS, ROWS = 32 * NRB;
+  static constexpr int BNS = KS == 1 ? 64 : 32, TK = KS * BNS, NJB = BNS / 32, NDB = D / 32;   // keys of a wave, of a tile
+  static constexpr int ROWB = D * 2, CH = D / 8, RP = 256 / ROWB, RPI = 1024 / ROWB;
+  static constexpr int TILE_B = TK * ROWB, BUF_B = 2 * TILE_B, NBUF = BUF_B * 4 <= 131072 ? 4 : 2, PD = NBUF - 1;
+  static constexpr int KI = TILE_B / 1024 / kManyWaves;   // loads per wave and tile
+  static constexpr int DBW = (NDB + KS - 1) / KS;         // 32-column blocks that a wave adds up
+  static constexpr int SLOT_F4 = NDB * 4 + 1;
+  static constexpr int COMB_B = KS > 1 ? kManyWaves * SLOT_F4 * 64 * 16 : 0;
+  static constexpr int SMEM_B = NBUF * BUF_B > COMB_B ? NBUF * BUF_B : COMB_B;
+  static constexpr int PART_FLOATS = ROWS * D + ROWS * 4;
+};
+
+template <class E, int D, int KS>
+__global__ __launch_bounds__(kManyWaves * 64, 2) void paged_many_kernel(const PagedParams p, int cus) {
+  using C = ManyCfg<D, KS>;
+  constexpr int NDB = C::NDB, NJB = C::NJB, BNS = C::BNS, TK = C::TK, KI = C::KI, PD = C::PD, NBUF = C::NBUF, NRB = C::NRB, DBW = C::DBW;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[C::SMEM_B];
+  __shared__ int32_t win[kWin];
+  __shared__ int first_bad, odd_from, role;
+
+  ManySpan sp;
+  if (!find_span<C::ROWS>(p, cus, sp)) return;
+  const Unit& u = sp.u;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rb = wave % NRB, ksp = wave / NRB;
+  const int row0 = u.tile * C::ROWS + rb * 32, tile_last = min((u.tile + 1) * C::ROWS, u.rows) - 1;
+  const bool wave_live = row0 < u.rows, ok = row0 + l32 < u.rows;
+  const int row = min(row0 + l32, u.rows - 1);
+  const int head = u.hk * p.G + row % p.G, token = u.start + row / p.G;
+  const int limit = limit_of(p, u, row);
+  const int seen = min(limit_of(p, u, tile_last), p.cap);
+  const int tile_all = limit_of(p, u, u.tile * C::ROWS), wave_all = limit_of(p, u, min(row0, u.rows - 1)), wave_any = limit_of(p, u, min(row0 + 31, u.rows - 1));
+  const int parts = seen <= sp.keys ? 1 : (seen - 1) / sp.keys + 1;
+  if (sp.part >= parts) return;
+  const int k0 = (int)min((int64_t)sp.part * sp.keys, (int64_t)seen), k1 = (int)min((int64_t)k0 + sp.keys, (int64_t)seen);
+
+  bf16x8_t qf[D / 16];
+  {
+    const uint16_t* qrow = p.q + token * p.qs[0] + head * p.qs[1];
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = as_bf16x8(*reinterpret_cast<const uint4*>(qrow + ks * 16 + hh * 8));
+  }
+  if (tid == 0) { first_bad = p.cap; odd_from = 0x7fffffff; }
+
+  const TileReads<D> rd(lane);
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void_t*)smem;
+  const unsigned char* const kbase = reinterpret_cast<const unsigned char*>(p.k + u.hk * p.cs[1]);
+  const unsigned char* const vbase = reinterpret_cast<const unsigned char*>(p.v + u.hk * p.cs[1]);
+  const int ld_row = wave * C::RPI + lane / C::CH, ld_pos = lane % C::CH;   // of load 0; later loads add 8 RPI rows
+  const int64_t page_b = p.cs[0] * 2, slot_b = p.cs[2] * 2;
+
+  RowState<D> st;
+  st.clear();
+  const int64_t wkeys = window_keys(p);
+  for (int64_t w0 = k0; w0 < k1; w0 += wkeys) {
+    const int w1 = (int)min(w0 + wkeys, (int64_t)k1);
+    __syncthreads();   // the last window's page numbers have been read (first time: first_bad is set)
+    fill_window(p, u.b, (int)w0, w1, win, &first_bad);
+    __syncthreads();
+    const int page0 = (int)page_of(p, (uint32_t)w0);
+    const int tiles = (w1 - (int)w0 + TK - 1) / TK;
+    auto issue = [&](int t) {
+      const uint32_t kl = lds + (t % NBUF) * C::BUF_B + wave * 1024, vl = kl + C::TILE_B;
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {
+        const int r = ld_row + i * 8 * C::RPI;
+        const int key = min((int)w0 + t * TK + r, w1 - 1);
+        const int pg = (int)page_of(p, key);
+        const int64_t off = win[pg - page0] * page_b + (key - pg * p.page_size) * slot_b;
+        load_to_lds_16(kbase + off + (ld_pos ^ ((r / C::RP) & (C::CH - 1))) * 16, kl + i * 8192);
+        load_to_lds_16(vbase + off + (ld_pos ^ (((r / C::RP) & (4 / C::RP - 1)) * 4)) * 16, vl + i * 8192);
+      }
+    };
+    wait_loads<0>();   // (whatever the compiler has in flight)
+#pragma unroll
+    for (int t = 0; t < PD; ++t)
+      if (t < tiles) issue(t);
+    for (int t = 0; t < tiles; ++t) {
+      const int later = min(PD - 1, tiles - 1 - t);
+      if (later >= 2) wait_loads<2 * 2 * KI>();
+      else if (later == 1) wait_loads<2 * KI>();
+      else wait_loads<0>();
+      const int t0 = (int)w0 + t * TK;
+      if (t0 + TK > min(tile_all, w1)) {
+#pragma unroll
+        for (int i = 0; i < KI; ++i) make_finite<E>(smem + (t % NBUF) * C::BUF_B + C::TILE_B + wave * 1024 + i * 8192 + lane * 16, t0, &odd_from);
+      }
+      __syncthreads();   // every wave's part of the tile is in LDS; everyone has finished the one before
+      if (t + PD < tiles) issue(t + PD);
+      const int j0 = t0 + ksp * BNS;
+      if (!wave_live || j0 >= min(wave_any, w1)) continue;
+      const unsigned char* const Kt = smem + (t % NBUF) * C::BUF_B + ksp * BNS * C::ROWB;
+      const bool masked = j0 + BNS > min(wave_all, w1);
+      floatx16_t s[NJB];
+      scores<E, D, NJB, D / 16 * NJB >= 16 ? 6 : 4>(Kt, rd, qf, s);
+      if (masked) mask_scores<NJB>(s, j0, min(limit, w1), hh);
+      uint4 pk[NJB][2];
+      softmax<E, D, NJB>(s, p.c, st, pk);
+      values<E, D, NJB>(Kt + C::TILE_B, rd, pk, st);
+    }
+  }
+  __syncthreads();   // first_bad and odd_from are final, and the tiles have been read
+  if (limit > first_bad) st.l = NAN;
+  if (ksp == 0) add_odd_values<E, D>(p, u, odd_from, min(limit, k1), hh, st);   // (behind a masked tile all are)
+
+  // ---- the key splits' results, added up in order: split j takes DBW column blocks from j DBW on
+  float m_all = st.m, l_tot;
+  floatx4_t acc[DBW * 4];
+  const int db0 = KS == 1 ? 0 : ksp * DBW;
+  if constexpr (KS == 1) {
+    l_tot = sum_with_other_half(st.l);
+#pragma unroll
+    for (int i = 0; i < DBW * 4; ++i) acc[i] = floatx4_t{st.o[i / 4][4 * (i % 4)], st.o[i / 4][4 * (i % 4) + 1], st.o[i / 4][4 * (i % 4) + 2], st.o[i / 4][4 * (i % 4) + 3]};
+  } else {
+    floatx4_t* const slots = reinterpret_cast<floatx4_t*>(smem);
+    floatx4_t* const mine = slots + wave * C::SLOT_F4 * 64 + lane;
+#pragma unroll
+    for (int i = 0; i < NDB * 4; ++i) mine[i * 64] = floatx4_t{st.o[i / 4][4 * (i % 4)], st.o[i / 4][4 * (i % 4) + 1], st.o[i / 4][4 * (i % 4) + 2], st.o[i / 4][4 * (i % 4) + 3]};
+    mine[NDB * 4 * 64] = floatx4_t{st.m, st.l, 0.f, 0.f};
+    __syncthreads();
+    float ms[KS], ls[KS], w[KS];
+    m_all = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const floatx4_t x = slots[((k * NRB + rb) * C::SLOT_F4 + NDB * 4) * 64 + lane];
+      ms[k] = x[0]; ls[k] = x[1];
+      m_all = fmaxf(m_all, x[0]);
+    }
+    const float m_ref = m_all == -INFINITY ? 0.f : m_all;
+    float l_all = 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      w[k] = fast_exp2(ms[k] - m_ref);
+      l_all += ls[k] * w[k];
+    }
+    l_tot = sum_with_other_half(l_all);
+#pragma unroll
+    for (int i = 0; i < DBW * 4; ++i) {
+      acc[i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+      if (db0 + i / 4 < NDB) {
+#pragma unroll
+        for (int k = 0; k < KS; ++k) acc[i] += slots[((k * NRB + rb) * C::SLOT_F4 + db0 * 4 + i) * 64 + lane] * w[k];
+      }
+    }
+  }
+  const bool has = wave_live && db0 < NDB;   // does this wave have columns of rows?
+
+  if (parts > 1) {
+    // park [row block][16-byte piece][lane], then (m, l) by [row block][lane]; of every kManyFan neighbours the last to arrive adds
+    // theirs up in the place of the first, and so on with these, until one has the result
+    constexpr uint32_t ML_AT = C::ROWS * D * 4, PART_B = C::PART_FLOATS * 4;
+    unsigned char* const first_slot = reinterpret_cast<unsigned char*>(p.parts) + (int64_t)sp.slot * PART_B;
+    const uint32_t at = (uint32_t)((rb * NDB + db0) * 4 * 64 + lane) * 16, ml_at = ML_AT + (uint32_t)(rb * 64 + lane) * 8;
+    auto park = [&](int part) {
+      if (!has) return;
+      const __amdgpu_buffer_rsrc_t buf = part_buffer(first_slot + (int64_t)part * PART_B);
+#pragma unroll
+      for (int i = 0; i < DBW * 4; ++i) store_part(buf, at + i * 1024, acc[i]);
+      if (ksp == 0) store_ml(buf, ml_at, m_all, l_tot);
+    };
+    park(sp.part);
+    int n = parts, idx = sp.part, stride = 1, level = 0;
+    for (;; ++level) {
+      const int g = idx / kManyFan, count = min(kManyFan, n - g * kManyFan), first = g * kManyFan * stride;
+      const bool last = n <= kManyFan;
+      if (count > 1) {   // (a single one is as it was)
+        wait_vmcnt<0>();
+        __syncthreads();   // every wave's stores are in memory
+        if (tid == 0) role = arrive(p.counters + (sp.slot + first) * kManyLevels + level, count);
+        __syncthreads();
+        if (role == kLeaves) return;
+        float2 s[kManyFan];
+        if (has) {
+          m_all = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < kManyFan; ++k) {
+            s[k] = make_float2(-INFINITY, 0.f);
+            if (k < count) s[k] = load_ml(part_buffer(first_slot + (int64_t)(first + k * stride) * PART_B), ml_at);
+            m_all = fmaxf(m_all, s[k].x);
+          }
+          const float m_ref = m_all == -INFINITY ? 0.f : m_all;
+          l_tot = 0.f;
+#pragma unroll
+          for (int i = 0; i < DBW * 4; ++i) acc[i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < kManyFan; ++k) {
+            if (k >= count) continue;
+            const __amdgpu_buffer_rsrc_t buf = part_buffer(first_slot + (int64_t)(first + k * stride) * PART_B);
+            const float w = fast_exp2(s[k].x - m_ref);
+            l_tot += s[k].y * w;
+#pragma unroll
+            for (int i = 0; i < DBW * 4; ++i) acc[i] += load_part(buf, at + i * 1024) * w;
+          }
+          if (role == kCountsWrong) l_tot = NAN;
+        }
+        if (!last) {
+          __syncthreads();   // (the other splits of the row block have read what is overwritten)
+          park(first);
+        }
+      }
+      if (last) break;
+      idx = g;
+      stride *= kManyFan;
+      n = (n + kManyFan - 1) / kManyFan;
+    }
+  }
+  if (!has || !ok) return;
+  const float inv = inverse_of(l_tot);
+#pragma unroll
+  for (int i = 0; i < DBW * 4; ++i)
+    if (db0 + i / 4 < NDB) store_out<E>(p, token, head, (db0 + i / 4) * 32 + 8 * (i % 4) + 4 * hh, make_float4(acc[i][0] * inv, acc[i][1] * inv, acc[i][2] * inv, acc[i][3] * inv));
+  if (ksp == 0 && hh == 0) p.lse[(int64_t)token * p.hq + head] = lse_of(m_all, l_tot);
+}
+
+int pick_splits(const loong_paged_desc& d, int cus) {
+  for (int ks = 1; ks < 4; ks *= 2)
+    if ((int64_t)d.n_tokens * d.n_q_heads >= (int64_t)(256 / ks) * cus) return ks;
+  return 4;
+}
+
+template <class E, int D>
+void launch(const PagedParams& p, int ks, int cus, unsigned grid, hipStream_t st) {
+  const dim3 g(grid), b(kManyWaves * 64);
+  if (ks == 1) paged_many_kernel<E, D, 1><<<g, b, 0, st>>>(p, cus);
+  else if (ks == 2) paged_many_kernel<E, D, 2><<<g, b, 0, st>>>(p, cus);
+  else paged_many_kernel<E, D, 4><<<g, b, 0, st>>>(p, cus);
+}
+
+}  // namespace
+
+// Spans of cut units are longer than load / (kManyMore cus) (0.999 of it: the sum is a float), so that there are at most kManyMore cus of
+// them and a remainder a unit, and at most as many units are cut.
+PagedPlan plan_paged_many(const loong_paged_desc& d, int cus) {
+  PagedPlan pl{};
+  const int rows = 256 / pick_splits(d, cus);
+  const int64_t group = d.n_q_heads / d.n_kv_heads;
+  const int64_t units = ((d.n_seqs < d.n_tokens ? d.n_seqs : d.n_tokens) + d.n_tokens * group / rows) * d.n_kv_heads;
+  const int64_t keys = cached_keys(d), parts = keys <= kManyLeast ? 1 : (keys + kManyLeast - 1) / kManyLeast;
+  const int64_t more = (int64_t)(kManyMore * cus * 1.01) + 8;
+  pl.workgroups = units + more;
+  if (units * parts < pl.workgroups) pl.workgroups = units * parts;
+  pl.workgroups = (pl.workgroups + 7) / 8 * 8;
+  pl.slots = parts == 1 ? 0 : 2 * more < pl.workgroups ? 2 * more : pl.workgroups;
+  pl.slot_floats = rows * (d.head_dim + 4);
+  return pl;
+}
+
+void launch_paged_many(const PagedParams& p, const loong_paged_desc& d, int cus, unsigned grid, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int ks = pick_splits(d, cus);
+  if (d.dtype == LOONG_BF16) {
+    if (d.head_dim == 128) launch<Bf16, 128>(p, ks, cus, grid, st);
+    else launch<Bf16, 64>(p, ks, cus, grid, st);
+  } else {
+    if (d.head_dim == 128) launch<Fp16, 128>(p, ks, cus, grid, st);
+    else launch<Fp16, 64>(p, ks, cus, grid, st);
+  }
+}
+
+}  // namespace loong
