@@ -35,6 +35,7 @@ int check_paged(const loong_paged_desc* d, int flags) {
       if (t.s[i] < 0 || t.s[i] > ((int64_t)1 << 40)) return fail(LOONG_E_SHAPE, "%s[%d] is negative or too large", t.name, i);
       if (t.s[i] % 8 != 0) return fail(LOONG_E_ALIGN, "%s[%d] = %lld is not a multiple of 8 elements", t.name, i, (long long)t.s[i]);
     }
+  if (d->cache_stride[2] >= ((int64_t)1 << 31)) return fail(LOONG_E_UNSUPPORTED, "slot strides must be below 2^31 elements");
   if (d->table_stride < 0 || d->table_stride > ((int64_t)1 << 40)) return fail(LOONG_E_SHAPE, "table_stride is negative or too large");
   return LOONG_OK;
 }

@@ -62,20 +62,31 @@ __device__ __forceinline__ void wait_loads() {
   static_assert(N >= 0 && N < 64, "vmcnt has six bits");
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// Before a loop over tiles: everything, also by the compiler's count, which else waits inside the loop for what it loaded before,
+// and with that for tiles in flight.
+__device__ __forceinline__ void wait_all_loads() {
+  wait_vmcnt<0>();
+  wait_loads<0>();
+}
 __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // ---- pages -----------------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t page_of(const PagedParams& p, uint32_t key) { return __umulhi(2 * key, p.page_mul) >> p.page_shift; }
+// Where a key's row begins, in bytes from its head's first; page0: the first page in `win`.  (A slot's stride is below 2^32 bytes.)
+__device__ __forceinline__ int64_t row_at(const PagedParams& p, const int64_t* win, int page0, int key) {
+  const uint32_t page = page_of(p, key), slot = key - page * p.page_size;
+  return win[(int)page - page0] + (int64_t)((uint64_t)slot * (uint32_t)(p.cs[2] * 2));
+}
 // keys whose pages are in LDS at a time
 __device__ __forceinline__ int64_t window_keys(const PagedParams& p) { return (int64_t)(kWin - 2) * p.page_size / 128 * 128; }
-// The workgroup's waves: pages of keys [k0, k1).  Barriers are the caller's.
-__device__ __forceinline__ void fill_window(const PagedParams& p, int b, int k0, int k1, int32_t* win, int* first_bad) {
+// The workgroup's waves: where the pages of keys [k0, k1) begin, in bytes.  Barriers are the caller's.
+__device__ __forceinline__ void fill_window(const PagedParams& p, int b, int k0, int k1, int64_t* win, int* first_bad) {
   const int p0 = (int)page_of(p, k0), n = (int)page_of(p, k1 - 1) - p0 + 1;
   for (int e = threadIdx.x; e < n; e += blockDim.x) {
     const int idx = p0 + e;
     const int page = idx < p.max_pages ? p.table[b * p.ts + idx] : -1;
     const bool ok = (uint32_t)page < (uint32_t)p.n_pages;
-    win[e] = ok ? page : 0;
+    win[e] = ok ? page * p.cs[0] * 2 : 0;
     if (!ok) atomicMin(first_bad, (int)min((int64_t)idx * p.page_size, (int64_t)0x7fffffff));
   }
 }
@@ -239,10 +250,11 @@ __device__ __forceinline__ void add_odd_values(const PagedParams& p, const Unit&
 
 template <int NJB>
 __device__ __forceinline__ void mask_scores(floatx16_t (&s)[NJB], int j0, int limit, int hh) {
+  const int left = limit - j0 - 4 * hh;   // keys of the tile that the row sees, from this half's first
 #pragma unroll
   for (int jb = 0; jb < NJB; ++jb)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) s[jb][v] = j0 + jb * 32 + acc_row(v, hh) < limit ? s[jb][v] : -INFINITY;
+    for (int v = 0; v < 16; ++v) s[jb][v] = jb * 32 + acc_row(v, 0) < left ? s[jb][v] : -INFINITY;
 }
 
 // ---- results ---------------------------------------------------------------------------------------------------

@@ -10,7 +10,7 @@
 // sequence, or a run of them).  Units of up to kShort grains are not cut: they are whole in the share that they begin in.  (48 sequences of
 // 1000 to 8192 keys, 8 kv heads, against spans of one length that the hardware deals out: FIG_BATCH us; two of 262144, one head: FIG_LONG.)
 //
-// A cut unit's shares are added up by the last to arrive (split_exchange.h), thirty-two at a time, so that a context spread over
+// A cut unit's shares are added up by the last to arrive (split_exchange.h), kFewFan at a time, so that a context spread over
 // the whole chip is not read by one workgroup.  (All 512 shares of a unit by one: 115 us for the two contexts above.)
 #include <hip/hip_runtime.h>
 
@@ -20,8 +20,8 @@ namespace loong {
 namespace {
 
 constexpr int kFewWaves = 4, kFewPerCu = 2;
-constexpr int kFewFan = 32;            // parts that are added up at a time
-constexpr int kFewLevels = 4;          // 32^4 parts are more than there are shares
+constexpr int kFewFan = 64;            // parts that are added up at a time
+constexpr int kFewLevels = 4;          // 64^4 parts are more than there are shares
 constexpr int kGrain = 64;             // keys that are not divided
 constexpr int kShort = 8;              // grains of a unit that is not divided, see above
 constexpr int kLeast = 4;              // grains of a share, at the least, of units that are
@@ -30,12 +30,13 @@ constexpr int kLeast = 4;              // grains of a share, at the least, of un
 // What a lane found out stays in LDS, where every wave writes the same and reads what it wrote.
 struct LineLanes {
   int here[64], upto[64];   // grains of a lane's sequences, and of all up to them
-  int start[64], n[64], rows[64], kv[64], grains[64];   // its sequence, if it has one
+  int start[64], n[64], rows[64], kv[64], grains[64], room[64];   // its sequence, if it has one; of a unit: its grains, and what it takes of the line
 };
 struct Line {
   int per;             // sequences a lane looks at
   int total, share;    // grains altogether, and of a share
   int shift;           // (0 unless a grain of 64 keys makes more than 2^29 of them)
+  bool apart;          // every unit begins with a share of its own
   LineLanes& lanes;
 
   static __device__ __forceinline__ int grains(const Seq& s, int shift) { return s.paged <= kGrain ? 1 : ((s.paged - 1) >> shift) / kGrain + 1; }
@@ -64,18 +65,38 @@ struct Line {
       all = wave_total(all);
       if (all < 5e8f || shift == 24) break;
     }
-    const int upto = wave_prefix(here);
-    lanes.here[lane] = here; lanes.upto[lane] = upto;
-    lanes.start[lane] = mine.start; lanes.n[lane] = mine.n; lanes.rows[lane] = mine.rows; lanes.kv[lane] = mine.kv;
-    lanes.grains[lane] = grains(mine, shift);
+    int upto = wave_prefix(here);
     total = all < 2e9f ? last_lane(upto) : 0;   // (so many units have no rows: seq_start decreases somewhere)
     most = wave_most(most);
     const int even = (total + (int)gridDim.x - 1) / (int)gridDim.x, least = most <= kShort ? most : kLeast;
     share = max(max(even, least), 1);
+    // where there are workgroups enough, no share has the end of one unit and the beginning of the next
+    apart = true;
+    int spread = 0;
+    float room = 0.f;
+    for (int i = 0; i < per; ++i) {
+      if (lane * per + i >= p.n_seqs) break;
+      const Seq s = per == 1 ? mine : sequence(p, lane * per + i);
+      if (s.rows == 0) continue;
+      const int n = room_of(grains(s, shift));
+      spread += n * p.hkv;
+      room += (float)n * (float)p.hkv;
+    }
+    apart = wave_total(room) <= (float)gridDim.x * (float)share;
+    if (apart) {
+      here = spread;
+      upto = wave_prefix(here);
+      total = last_lane(upto);
+    }
+    lanes.here[lane] = here; lanes.upto[lane] = upto;
+    lanes.start[lane] = mine.start; lanes.n[lane] = mine.n; lanes.rows[lane] = mine.rows; lanes.kv[lane] = mine.kv;
+    lanes.grains[lane] = grains(mine, shift); lanes.room[lane] = room_of(grains(mine, shift));
   }
 
-  // the unit at `pos` (below total), its first grain and its grains
-  __device__ __forceinline__ Unit at(const PagedParams& p, int pos, int& start, int& n) const {
+  __device__ __forceinline__ int room_of(int n) const { return !apart ? n : n <= kShort ? share : (int)((uint32_t)(n + share - 1) / (uint32_t)share) * share; }
+
+  // the unit at `pos` (below total), its first grain, its grains and what it takes of the line
+  __device__ __forceinline__ Unit at(const PagedParams& p, int pos, int& start, int& n, int& room) const {
     const int lane = threadIdx.x & 63;
     const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lanes.upto[lane] > pos));
     int before = __builtin_amdgcn_readfirstlane(lanes.upto[l] - lanes.here[l]);
@@ -84,13 +105,13 @@ struct Line {
       u.b = l;
       u.start = __builtin_amdgcn_readfirstlane(lanes.start[l]); u.n = __builtin_amdgcn_readfirstlane(lanes.n[l]);
       u.rows = __builtin_amdgcn_readfirstlane(lanes.rows[l]); u.kv = __builtin_amdgcn_readfirstlane(lanes.kv[l]);
-      n = __builtin_amdgcn_readfirstlane(lanes.grains[l]);
+      n = __builtin_amdgcn_readfirstlane(lanes.grains[l]); room = __builtin_amdgcn_readfirstlane(lanes.room[l]);
     } else {
       for (int i = 0;; i += 64) {   // (ends: the run has the grain)
         const int b = l * per + i + lane;
         Seq s{};
         if (i + lane < per && b < p.n_seqs) s = sequence(p, b);
-        const int g = s.rows ? grains(s, shift) * p.hkv : 0, sum = wave_prefix(g);
+        const int g = s.rows ? room_of(grains(s, shift)) * p.hkv : 0, sum = wave_prefix(g);
         const uint64_t past = __builtin_amdgcn_ballot_w64(before + sum > pos);
         if (past || i + 64 >= per) {
           const int from = past ? __builtin_ctzll(past) : 63;
@@ -98,15 +119,15 @@ struct Line {
           u.b = __builtin_amdgcn_readlane(b, from);
           u.start = __builtin_amdgcn_readlane(s.start, from); u.n = __builtin_amdgcn_readlane(s.n, from);
           u.rows = __builtin_amdgcn_readlane(s.rows, from); u.kv = __builtin_amdgcn_readlane(s.kv, from);
-          n = __builtin_amdgcn_readlane(grains(s, shift), from);
+          n = __builtin_amdgcn_readlane(grains(s, shift), from); room = room_of(n);
           break;
         }
         before += last_lane(sum);
       }
     }
-    u.hk = (int)((uint32_t)(pos - before) / (uint32_t)n);
+    u.hk = (int)((uint32_t)(pos - before) / (uint32_t)room);
     u.tile = 0;
-    start = before + u.hk * n;
+    start = before + u.hk * room;
     return u;
   }
 };
@@ -128,7 +149,7 @@ struct FewCfg {
 template <class E, int D>
 struct FewShared {
   __attribute__((aligned(1024))) unsigned char smem[kFewWaves * FewCfg<D>::WAVE_B];
-  int32_t win[kWin];
+  int64_t win[kWin];
   float2 ml[kFewWaves][64];
   int first_bad, odd_from, role;
   LineLanes lanes;
@@ -162,7 +183,6 @@ __device__ __forceinline__ void few_keys(const PagedParams& p, const Unit& u, in
   const unsigned char* const kbase = reinterpret_cast<const unsigned char*>(p.k + u.hk * p.cs[1]);
   const unsigned char* const vbase = reinterpret_cast<const unsigned char*>(p.v + u.hk * p.cs[1]);
   const int ld_row = lane / C::CH, ld_pos = lane % C::CH;
-  const int64_t page_b = p.cs[0] * 2, slot_b = p.cs[2] * 2;
 
   const int64_t wkeys = window_keys(p);
   for (int64_t w0 = k0; w0 < k1; w0 += wkeys) {
@@ -177,8 +197,7 @@ __device__ __forceinline__ void few_keys(const PagedParams& p, const Unit& u, in
 #pragma unroll
       for (int i = 0; i < C::LI; ++i) {
         const int key = min((int)w0 + t * BNS + i * C::RPI + ld_row, w1 - 1);
-        const int pg = (int)page_of(p, key);
-        off[i] = win[pg - page0] * page_b + (key - pg * p.page_size) * slot_b;
+        off[i] = row_at(p, win, page0, key);
       }
     };
     auto issue_k = [&] {
@@ -196,7 +215,7 @@ __device__ __forceinline__ void few_keys(const PagedParams& p, const Unit& u, in
       }
     };
     int t = wave;
-    wait_loads<0>();   // (whatever the compiler has in flight)
+    wait_all_loads();
     if (t < tiles) { place(t); issue_k(); issue_v(); }
     for (; t < tiles; t += kFewWaves) {
       const int j0 = (int)w0 + t * BNS;
@@ -368,14 +387,14 @@ __global__ __launch_bounds__(kFewWaves * 64, kFewPerCu) void paged_few_kernel(co
   const int end = min(pos + line.share, line.total);
   bool again = false;
   while (pos < end) {
-    int start, n;
-    const Unit u = line.at(p, pos, start, n);
+    int start, n, room;
+    const Unit u = line.at(p, pos, start, n, room);
     const int seen = min(limit_of(p, u, u.rows - 1), p.cap), grain = kGrain << line.shift;
     const int seen_n = max((int)(((int64_t)seen + grain - 1) / grain), 1);   // grains that any row sees
     Part part{0, 1, 0, 0};
-    int to = start + n;
+    int to = start + room;
     if (n <= kShort) {
-      if (pos > start) { pos = to; continue; }   // (the share before has it)
+      if (pos > start) { pos = to; continue; }   // (the share that it begins in has it)
     } else {
       to = min(to, end);
       const int first = start / line.share, last = (start + seen_n - 1) / line.share;
@@ -385,7 +404,7 @@ __global__ __launch_bounds__(kFewWaves * 64, kFewPerCu) void paged_few_kernel(co
       part.slot1 = 2 * first + 2;
     }
     if (part.part < part.parts) {
-      const int k0 = (int)min((int64_t)(pos - start) * grain, (int64_t)seen), k1 = (int)min((int64_t)(to - start) * grain, (int64_t)seen);
+      const int k0 = (int)min((int64_t)(pos - start) * grain, (int64_t)seen), k1 = n <= kShort ? seen : (int)min((int64_t)(to - start) * grain, (int64_t)seen);
       if (again) __syncthreads();   // the unit before is done with LDS
       again = true;
       RowState<D> st;

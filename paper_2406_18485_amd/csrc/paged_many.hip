@@ -2,12 +2,14 @@
 //
 // Bound by the matrix cores and what feeds them, like the forward step (attn_fwd.hip), whose loop this is: eight waves = 8 / KS blocks
 // of 32 rows x KS key splits; a tile of K and V is staged for all of them, several tiles deep.  The query rows of a kv head (token by
-// token, the group's q heads of each) are cut into tiles of 256 / KS; KS is the smallest that gives every unit of the chip a tile (fewer
-// rows a workgroup read the same keys more often, but are more workgroups without an exchange between them).
+// token, the group's q heads of each) are cut into tiles of 256 / KS.
 //
-// Division.  A unit (sequence, kv head, row tile) is cut into spans of keys where that shortens the launch.  The lengths are in
-// device memory: every wave works out, for a few lengths of a span, how many spans there would be and about how long they would
-// take, and all take the best one.  A cut unit's spans are added up by the last to arrive (split_exchange.h), kManyFan at a time.
+// Division.  A unit (sequence, kv head, row tile) may be cut into spans of keys, which are added up by the last of them to arrive
+// (split_exchange.h), kManyFan at a time.  Whole units of 256 rows use the matrix cores best (KS = 1: 1030 to 1090 TFLOP/s over long contexts,
+// KS = 4 640 to 710), but where they are fewer than the chip's units either they are cut, which costs an exchange of 128 KB a span, or the
+// row tiles are made smaller.  Which is faster goes by the lengths, which are in device memory: every wave works out, for both and for
+// a few lengths of a span, how many spans there would be and about how long they would take, and all take the best.  (1000 tokens, 8
+// heads on 2, KS = 1 / KS = 4: over 1000 keys 27 / 22 us, 6000 53 / 54, 16000 90 / 110, 64000 271 / 365.)
 #include <hip/hip_runtime.h>
 
 #include "paged_body.h"
@@ -19,74 +21,110 @@ constexpr int kManyWaves = 8;
 constexpr int kManyFan = 4;            // parts that are added up at a time
 constexpr int kManyLevels = 6;         // 4^6 parts are more than a unit has
 constexpr int kManyLeast = 256;        // keys of a span of a cut unit, at the least
-constexpr int kManyFixed = 512;        // what a span costs besides its keys, in keys
 constexpr int kManyMore = 2;           // spans that cutting may add, per unit of the chip
+// what a span takes, in ns: per key; whatever it has; more if its unit is cut (from the times above)
+constexpr float kKeyNs[2] = {32.f, 12.f}, kFixedNs[2] = {9000.f, 8000.f}, kCutNs[2] = {9000.f, 4000.f};   // KS = 1, 4
 
+struct ManyArgs {
+  int cus;
+  int units;    // that there can be, at the most
+};
+
+// How all the work is divided: rows of a tile, keys of a span, spans.
+struct Division {
+  int rows, keys, all;
+};
 struct ManySpan {
   Unit u;
-  int keys, part;
+  int part;
   int slot;                // number of the unit's first span among those of all cut units
 };
 
-// Every wave for itself: a lane looks at sequences lane, lane + 64, ...
-template <int ROWS>
-__device__ __forceinline__ bool find_span(const PagedParams& p, int cus, ManySpan& out) {
-  const int lane = threadIdx.x & 63;
-  auto tiles_of = [&](const Seq& s) { return (s.rows + ROWS - 1) / ROWS; };
-  auto parts_of = [](const Seq& s, int keys) { return s.paged <= keys ? 1 : (int)((uint32_t)(s.paged - 1) / (uint32_t)keys) + 1; };
-  Seq mine{};
-  if (lane < p.n_seqs) mine = sequence(p, lane);
-  auto seq_at = [&](int base) {
+// The sequences, 64 at a time: a lane looks at base + lane.
+struct Lanes {
+  Seq mine;
+  __device__ __forceinline__ Lanes(const PagedParams& p) : mine{} {
+    const int lane = threadIdx.x & 63;
+    if (lane < p.n_seqs) mine = sequence(p, lane);
+  }
+  __device__ __forceinline__ Seq at(const PagedParams& p, int base) const {
     Seq s = mine;
     if (base > 0) {
+      const int b = base + (threadIdx.x & 63);
       s = Seq{};
-      if (base + lane < p.n_seqs) s = sequence(p, base + lane);
+      if (b < p.n_seqs) s = sequence(p, b);
     }
     return s;
-  };
-  float load = 0.f, units = 0.f;
+  }
+};
+__device__ __forceinline__ int tiles_of(const Seq& s, int rows) { return (s.rows + rows - 1) >> (rows == 64 ? 6 : 8); }
+__device__ __forceinline__ int parts_of(const Seq& s, int keys) { return s.paged <= keys ? 1 : (int)((uint32_t)(s.paged - 1) / (uint32_t)keys) + 1; }
+
+// (Estimates in floats: an integer division is some 40 instructions, and all this is in front of the first load of a key.)
+template <bool BOTH>
+__device__ __forceinline__ Division divide(const PagedParams& p, const ManyArgs& a, const Lanes& lanes) {
+  Division d{256, 0, 0};
+  float best = INFINITY;
+  const float cus = (float)a.cus, per_unit = __builtin_amdgcn_rcpf(cus);
   int most = 0;
   for (int base = 0; base < p.n_seqs; base += 64) {
-    const Seq s = seq_at(base);
-    const int t = tiles_of(s);
-    load += (float)t * (float)s.paged;
-    units += (float)t;
-    most = max(most, t ? s.paged : 0);
+    const Seq s = lanes.at(p, base);
+    most = max(most, s.rows ? s.paged : 0);
   }
-  load = wave_total(load) * p.hkv;
-  units = wave_total(units) * p.hkv;
   most = wave_most(most);
-  if (units == 0.f || units > (float)gridDim.x) return false;   // (more than there can be: seq_start decreases somewhere)
-  // the span that ends first: all alike, in rounds; unequal, in what is left of a unit of the chip after equal work
-  const float per_cu = load / cus;
-  const int fit = (int)(cus / units);   // parts that give every unit of the chip one
-  int keys = 0, all = 0;
-  float best = INFINITY;
-#pragma unroll 1
-  for (int c = 0; c < 6; ++c) {
-    const int cut = c < 4 ? (c + 1) * max(fit, 1) : 1;
-    int k = c < 4 ? (int)(((int64_t)most + cut - 1) / cut) : c == 4 ? (int)fminf(per_cu, 2e9f) : (int)fminf(0.5f * per_cu, 2e9f);
-    k = max(k < 0x7fffff00 ? (k + 63) / 64 * 64 : k, kManyLeast);
-    // (what bounds the number of spans, and their slots: cutting adds at most kManyMore a unit of the chip)
-    if (load > (float)k * (float)(kManyMore * cus) * 0.999f && k < most) continue;
-    int n = 0;
+#pragma unroll
+  for (int small = 0; small < (BOTH ? 2 : 1); ++small) {
+    const int rows = small ? 64 : 256;
+    float load = 0.f, units = 0.f;
     for (int base = 0; base < p.n_seqs; base += 64) {
-      const Seq s = seq_at(base);
-      n += tiles_of(s) * parts_of(s, k);
+      const Seq s = lanes.at(p, base);
+      const float t = (float)tiles_of(s, rows);
+      load += t * (float)s.paged;
+      units += t;
     }
-    n = wave_total(n) * p.hkv;
-    const float cost = k >= most ? (float)most : (float)k;
-    const float rounds = (float)((n + cus - 1) / cus), est = 0.5f * (rounds * (cost + kManyFixed) + per_cu + (float)n / cus * kManyFixed);
-    if (est < best) { best = est; keys = k; all = n; }
+    load = wave_total(load) * p.hkv;
+    units = wave_total(units) * p.hkv;
+    if (units == 0.f || units > (float)a.units) return Division{256, 1, 0};   // (more than there can be: seq_start decreases somewhere)
+    // not cut; cut so that every unit of the chip has a span of the longest; cut into equal work
+    const float even = load * per_unit, fit = floorf(cus * __builtin_amdgcn_rcpf(units) + 1e-3f);
+#pragma unroll 1
+    for (int c = 0; c < 3; ++c) {
+      if (c == 1 && fit < 2.f) continue;
+      const float want = c == 0 ? (float)most : c == 1 ? (float)most * __builtin_amdgcn_rcpf(fit) + 1.f : even;
+      int k = want < 2e9f ? ((int)want + 63) / 64 * 64 : most;
+      k = max(k, kManyLeast);
+      if (c > 0 && k >= most) continue;
+      // (what bounds the number of spans, and their slots: cutting adds at most kManyMore a unit of the chip)
+      if (k < most && load > (float)k * (kManyMore * 0.999f) * cus) continue;
+      float n = units;
+      if (k < most) {
+        const float inv = __builtin_amdgcn_rcpf((float)k);
+        n = 0.f;
+        for (int base = 0; base < p.n_seqs; base += 64) {
+          const Seq s = lanes.at(p, base);
+          n += (float)tiles_of(s, rows) * fmaxf(ceilf((float)s.paged * inv - 1e-4f), 1.f);
+        }
+        n = wave_total(n) * p.hkv;
+      }
+      // all alike, in rounds; unequal, in equal work and the longest at the least
+      const float fixed = kFixedNs[small] + (k < most ? kCutNs[small] : 0.f), span = (float)min(k, most) * kKeyNs[small] + fixed;
+      const float est = 0.5f * (ceilf(n * per_unit - 1e-3f) * span + fmaxf((load * kKeyNs[small] + n * fixed) * per_unit, span));
+      if (est < best) { best = est; d.rows = rows; d.keys = k; }
+    }
   }
-  if (keys == 0 || all > (int)gridDim.x) return false;   // (never: not to cut at all is always among them)
-  // neighbours share an XCD and its L2 where they read the same keys
-  const int per = (all + 7) / 8, idx = blockIdx.x >> 3, item = (int)(blockIdx.x & 7) * per + idx;
-  if (idx >= per || item >= all) return false;
+  for (int base = 0; base < p.n_seqs; base += 64) {
+    const Seq s = lanes.at(p, base);
+    d.all += tiles_of(s, d.rows) * parts_of(s, d.keys);
+  }
+  d.all = wave_total(d.all) * p.hkv;
+  return d;
+}
+
+__device__ __forceinline__ bool find_span(const PagedParams& p, const Division& d, const Lanes& lanes, int item, ManySpan& out) {
   int before = 0, slot = 0;
   for (int base = 0; base < p.n_seqs; base += 64) {
-    const Seq s = seq_at(base);
-    const int parts = parts_of(s, keys), n = tiles_of(s) * parts * p.hkv, cut = parts > 1 ? n : 0;
+    const Seq s = lanes.at(p, base);
+    const int parts = parts_of(s, d.keys), n = tiles_of(s, d.rows) * parts * p.hkv, cut = parts > 1 ? n : 0;
     const int upto = wave_prefix(n), slots = wave_prefix(cut);
     const uint64_t past = __builtin_amdgcn_ballot_w64(before + upto > item);
     if (past) {
@@ -95,8 +133,7 @@ __device__ __forceinline__ bool find_span(const PagedParams& p, int cus, ManySpa
       out.u.b = base + l;
       out.u.start = __builtin_amdgcn_readlane(s.start, l); out.u.n = __builtin_amdgcn_readlane(s.n, l);
       out.u.rows = __builtin_amdgcn_readlane(s.rows, l); out.u.kv = __builtin_amdgcn_readlane(s.kv, l);
-      const int np = __builtin_amdgcn_readlane(parts, l), nt = (out.u.rows + ROWS - 1) / ROWS;
-      out.keys = keys;
+      const int np = __builtin_amdgcn_readlane(parts, l), nt = (out.u.rows + d.rows - 1) >> (d.rows == 64 ? 6 : 8);
       out.u.hk = at / (np * nt);
       const int rest = at - out.u.hk * np * nt;
       out.part = rest / nt;
@@ -124,19 +161,21 @@ struct ManyCfg {
   static constexpr int PART_FLOATS = ROWS * D + ROWS * 4;
 };
 
+struct ManyShared {
+  int64_t win[kWin];
+  int first_bad, odd_from, role;
+};
+
+// One span.  (The lane is counted anew: what derives from it would else be kept in registers from span to span.)
 template <class E, int D, int KS>
-__global__ __launch_bounds__(kManyWaves * 64, 2) void paged_many_kernel(const PagedParams p, int cus) {
+__device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& sp, int keys, unsigned char* smem, ManyShared& sh) {
   using C = ManyCfg<D, KS>;
   constexpr int NDB = C::NDB, NJB = C::NJB, BNS = C::BNS, TK = C::TK, KI = C::KI, PD = C::PD, NBUF = C::NBUF, NRB = C::NRB, DBW = C::DBW;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[C::SMEM_B];
-  __shared__ int32_t win[kWin];
-  __shared__ int first_bad, odd_from, role;
-
-  ManySpan sp;
-  if (!find_span<C::ROWS>(p, cus, sp)) return;
+  int64_t* const win = sh.win;
+  int &first_bad = sh.first_bad, &odd_from = sh.odd_from, &role = sh.role;
   const Unit& u = sp.u;
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rb = wave % NRB, ksp = wave / NRB;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rb = wave % NRB, ksp = wave / NRB;
+  const int lane = lane_again(), l32 = lane & 31, hh = lane >> 5, tid = wave * 64 + lane;
   const int row0 = u.tile * C::ROWS + rb * 32, tile_last = min((u.tile + 1) * C::ROWS, u.rows) - 1;
   const bool wave_live = row0 < u.rows, ok = row0 + l32 < u.rows;
   const int row = min(row0 + l32, u.rows - 1);
@@ -144,9 +183,9 @@ __global__ __launch_bounds__(kManyWaves * 64, 2) void paged_many_kernel(const Pa
   const int limit = limit_of(p, u, row);
   const int seen = min(limit_of(p, u, tile_last), p.cap);
   const int tile_all = limit_of(p, u, u.tile * C::ROWS), wave_all = limit_of(p, u, min(row0, u.rows - 1)), wave_any = limit_of(p, u, min(row0 + 31, u.rows - 1));
-  const int parts = seen <= sp.keys ? 1 : (seen - 1) / sp.keys + 1;
+  const int parts = seen <= keys ? 1 : (seen - 1) / keys + 1;
   if (sp.part >= parts) return;
-  const int k0 = (int)min((int64_t)sp.part * sp.keys, (int64_t)seen), k1 = (int)min((int64_t)k0 + sp.keys, (int64_t)seen);
+  const int k0 = (int)min((int64_t)sp.part * keys, (int64_t)seen), k1 = (int)min((int64_t)k0 + keys, (int64_t)seen);
 
   bf16x8_t qf[D / 16];
   {
@@ -161,7 +200,6 @@ __global__ __launch_bounds__(kManyWaves * 64, 2) void paged_many_kernel(const Pa
   const unsigned char* const kbase = reinterpret_cast<const unsigned char*>(p.k + u.hk * p.cs[1]);
   const unsigned char* const vbase = reinterpret_cast<const unsigned char*>(p.v + u.hk * p.cs[1]);
   const int ld_row = wave * C::RPI + lane / C::CH, ld_pos = lane % C::CH;   // of load 0; later loads add 8 RPI rows
-  const int64_t page_b = p.cs[0] * 2, slot_b = p.cs[2] * 2;
 
   RowState<D> st;
   st.clear();
@@ -179,13 +217,12 @@ __global__ __launch_bounds__(kManyWaves * 64, 2) void paged_many_kernel(const Pa
       for (int i = 0; i < KI; ++i) {
         const int r = ld_row + i * 8 * C::RPI;
         const int key = min((int)w0 + t * TK + r, w1 - 1);
-        const int pg = (int)page_of(p, key);
-        const int64_t off = win[pg - page0] * page_b + (key - pg * p.page_size) * slot_b;
+        const int64_t off = row_at(p, win, page0, key);
         load_to_lds_16(kbase + off + (ld_pos ^ ((r / C::RP) & (C::CH - 1))) * 16, kl + i * 8192);
         load_to_lds_16(vbase + off + (ld_pos ^ (((r / C::RP) & (4 / C::RP - 1)) * 4)) * 16, vl + i * 8192);
       }
     };
-    wait_loads<0>();   // (whatever the compiler has in flight)
+    wait_all_loads();
 #pragma unroll
     for (int t = 0; t < PD; ++t)
       if (t < tiles) issue(t);
@@ -296,14 +333,22 @@ __global__ __launch_bounds__(kManyWaves * 64, 2) void paged_many_kernel(const Pa
           l_tot = 0.f;
 #pragma unroll
           for (int i = 0; i < DBW * 4; ++i) acc[i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+          // (a part's pieces all at once, and the next one's while they are added)
+          floatx4_t x[2][DBW * 4];
+          auto ask = [&](int k) {
+            const __amdgpu_buffer_rsrc_t buf = part_buffer(first_slot + (int64_t)(first + min(k, count - 1) * stride) * PART_B);
+#pragma unroll
+            for (int i = 0; i < DBW * 4; ++i) x[k % 2][i] = load_part(buf, at + i * 1024);
+          };
+          ask(0);
 #pragma unroll
           for (int k = 0; k < kManyFan; ++k) {
+            if (k + 1 < kManyFan) ask(k + 1);
             if (k >= count) continue;
-            const __amdgpu_buffer_rsrc_t buf = part_buffer(first_slot + (int64_t)(first + k * stride) * PART_B);
             const float w = fast_exp2(s[k].x - m_ref);
             l_tot += s[k].y * w;
 #pragma unroll
-            for (int i = 0; i < DBW * 4; ++i) acc[i] += load_part(buf, at + i * 1024) * w;
+            for (int i = 0; i < DBW * 4; ++i) acc[i] += x[k % 2][i] * w;
           }
           if (role == kCountsWrong) l_tot = NAN;
         }
@@ -326,48 +371,72 @@ __global__ __launch_bounds__(kManyWaves * 64, 2) void paged_many_kernel(const Pa
   if (ksp == 0 && hh == 0) p.lse[(int64_t)token * p.hq + head] = lse_of(m_all, l_tot);
 }
 
-int pick_splits(const loong_paged_desc& d, int cus) {
-  for (int ks = 1; ks < 4; ks *= 2)
-    if ((int64_t)d.n_tokens * d.n_q_heads >= (int64_t)(256 / ks) * cus) return ks;
-  return 4;
+// BOTH: row tiles of 64 too; with every unit of the chip holding one workgroup, which goes on from span to span.
+template <class E, int D, bool BOTH>
+__global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void paged_many_kernel(const PagedParams p, const ManyArgs a) {
+  constexpr int BYTES = BOTH && ManyCfg<D, 4>::SMEM_B > ManyCfg<D, 1>::SMEM_B ? ManyCfg<D, 4>::SMEM_B : ManyCfg<D, 1>::SMEM_B;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[BYTES];
+  __shared__ ManyShared sh;
+  const Lanes lanes(p);
+  const Division d = divide<BOTH>(p, a, lanes);
+  // neighbours share an XCD and its L2 where they read the same keys
+  const int per = (d.all + 7) / 8, xcd = blockIdx.x & 7;
+  bool again = false;
+  for (int idx = blockIdx.x >> 3; idx < per; idx += gridDim.x >> 3) {
+    ManySpan sp;
+    const int item = xcd * per + idx;
+    if (item >= d.all || !find_span(p, d, lanes, item, sp)) break;
+    if (again) __syncthreads();   // the span before is done with LDS
+    again = true;
+    if (!BOTH || d.rows == 256) many_span<E, D, 1>(p, sp, d.keys, smem, sh);
+    else if constexpr (BOTH) many_span<E, D, 4>(p, sp, d.keys, smem, sh);
+  }
+}
+
+// Are there row tiles of 256 for every unit of the chip?
+bool rows_fill(const loong_paged_desc& d, int cus) { return (int64_t)d.n_tokens * d.n_q_heads >= (int64_t)256 * cus; }
+int64_t most_units(const loong_paged_desc& d, int rows) {
+  const int64_t group = d.n_q_heads / d.n_kv_heads;
+  return ((d.n_seqs < d.n_tokens ? d.n_seqs : d.n_tokens) + d.n_tokens * group / rows) * d.n_kv_heads;
 }
 
 template <class E, int D>
-void launch(const PagedParams& p, int ks, int cus, unsigned grid, hipStream_t st) {
+void launch(const PagedParams& p, bool both, const ManyArgs& a, unsigned grid, hipStream_t st) {
   const dim3 g(grid), b(kManyWaves * 64);
-  if (ks == 1) paged_many_kernel<E, D, 1><<<g, b, 0, st>>>(p, cus);
-  else if (ks == 2) paged_many_kernel<E, D, 2><<<g, b, 0, st>>>(p, cus);
-  else paged_many_kernel<E, D, 4><<<g, b, 0, st>>>(p, cus);
+  if (both) paged_many_kernel<E, D, true><<<g, b, 0, st>>>(p, a);
+  else paged_many_kernel<E, D, false><<<g, b, 0, st>>>(p, a);
 }
 
 }  // namespace
 
+// Where row tiles of 256 fill the chip the hardware deals the spans out, else as many workgroups as it holds take them in turn.
 // Spans of cut units are longer than load / (kManyMore cus) (0.999 of it: the sum is a float), so that there are at most kManyMore cus of
 // them and a remainder a unit, and at most as many units are cut.
 PagedPlan plan_paged_many(const loong_paged_desc& d, int cus) {
   PagedPlan pl{};
-  const int rows = 256 / pick_splits(d, cus);
-  const int64_t group = d.n_q_heads / d.n_kv_heads;
-  const int64_t units = ((d.n_seqs < d.n_tokens ? d.n_seqs : d.n_tokens) + d.n_tokens * group / rows) * d.n_kv_heads;
+  const bool both = !rows_fill(d, cus);
+  const int64_t units = most_units(d, both ? 64 : 256);
   const int64_t keys = cached_keys(d), parts = keys <= kManyLeast ? 1 : (keys + kManyLeast - 1) / kManyLeast;
   const int64_t more = (int64_t)(kManyMore * cus * 1.01) + 8;
-  pl.workgroups = units + more;
-  if (units * parts < pl.workgroups) pl.workgroups = units * parts;
+  int64_t spans = units + more;
+  if (units * parts < spans) spans = units * parts;
+  pl.workgroups = both && spans > cus ? cus : spans;
   pl.workgroups = (pl.workgroups + 7) / 8 * 8;
-  pl.slots = parts == 1 ? 0 : 2 * more < pl.workgroups ? 2 * more : pl.workgroups;
-  pl.slot_floats = rows * (d.head_dim + 4);
+  pl.slots = parts == 1 ? 0 : 2 * more < spans ? 2 * more : spans;
+  pl.slot_floats = 256 * (d.head_dim + 4);
   return pl;
 }
 
 void launch_paged_many(const PagedParams& p, const loong_paged_desc& d, int cus, unsigned grid, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const int ks = pick_splits(d, cus);
+  const bool both = !rows_fill(d, cus);
+  const ManyArgs a{cus, (int)most_units(d, both ? 64 : 256)};
   if (d.dtype == LOONG_BF16) {
-    if (d.head_dim == 128) launch<Bf16, 128>(p, ks, cus, grid, st);
-    else launch<Bf16, 64>(p, ks, cus, grid, st);
+    if (d.head_dim == 128) launch<Bf16, 128>(p, both, a, grid, st);
+    else launch<Bf16, 64>(p, both, a, grid, st);
   } else {
-    if (d.head_dim == 128) launch<Fp16, 128>(p, ks, cus, grid, st);
-    else launch<Fp16, 64>(p, ks, cus, grid, st);
+    if (d.head_dim == 128) launch<Fp16, 128>(p, both, a, grid, st);
+    else launch<Fp16, 64>(p, both, a, grid, st);
   }
 }
 

@@ -6,7 +6,7 @@
 
 namespace loong {
 
-constexpr int kWin = 2048;             // page numbers in LDS
+constexpr int kWin = 1024;             // pages whose places are in LDS
 constexpr int kFewRows = 32;           // query rows of a kv head up to which the kernel for few is taken
 
 struct PagedParams {
