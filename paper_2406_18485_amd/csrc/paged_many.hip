@@ -12,6 +12,8 @@
 // heads on 2, KS = 1 / KS = 4: over 1000 keys 27 / 22 us, 6000 53 / 54, 16000 90 / 110, 64000 271 / 365.)
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "paged_body.h"
 
 namespace loong {
@@ -22,8 +24,9 @@ constexpr int kManyFan = 4;            // parts that are added up at a time
 constexpr int kManyLevels = 6;         // 4^6 parts are more than a unit has
 constexpr int kManyLeast = 256;        // keys of a span of a cut unit, at the least
 constexpr int kManyMore = 2;           // spans that cutting may add, per unit of the chip
-// what a span takes, in ns: per key; whatever it has; more if its unit is cut (from the times above)
-constexpr float kKeyNs[2] = {32.f, 12.f}, kFixedNs[2] = {9000.f, 8000.f}, kCutNs[2] = {9000.f, 4000.f};   // KS = 1, 4
+// What a span takes, in ns: per key at head_dim 128 (KS = 1, 2, 4; 0.7 of it at 64) and whatever it has; if its unit is cut, every level of
+// adding parts up takes its waits, and every part that is added what one workgroup needs to read it (50 bytes a ns).
+constexpr float kKeyNs[3] = {31.5f, 18.5f, 12.f}, kFixedNs = 9500.f, kCutNs = 1500.f, kLevelNs = 1500.f, kPartNs = 0.08f;
 
 struct ManyArgs {
   int cus;
@@ -57,11 +60,11 @@ struct Lanes {
     return s;
   }
 };
-__device__ __forceinline__ int tiles_of(const Seq& s, int rows) { return (s.rows + rows - 1) >> (rows == 64 ? 6 : 8); }
+__device__ __forceinline__ int tiles_of(const Seq& s, int rows) { return (s.rows + rows - 1) >> (rows == 64 ? 6 : rows == 128 ? 7 : 8); }
 __device__ __forceinline__ int parts_of(const Seq& s, int keys) { return s.paged <= keys ? 1 : (int)((uint32_t)(s.paged - 1) / (uint32_t)keys) + 1; }
 
 // (Estimates in floats: an integer division is some 40 instructions, and all this is in front of the first load of a key.)
-template <bool BOTH>
+template <bool BOTH, int D>
 __device__ __forceinline__ Division divide(const PagedParams& p, const ManyArgs& a, const Lanes& lanes) {
   Division d{256, 0, 0};
   float best = INFINITY;
@@ -73,8 +76,8 @@ __device__ __forceinline__ Division divide(const PagedParams& p, const ManyArgs&
   }
   most = wave_most(most);
 #pragma unroll
-  for (int small = 0; small < (BOTH ? 2 : 1); ++small) {
-    const int rows = small ? 64 : 256;
+  for (int small = 0; small < (BOTH ? 3 : 1); ++small) {
+    const int rows = 256 >> small;
     float load = 0.f, units = 0.f;
     for (int base = 0; base < p.n_seqs; base += 64) {
       const Seq s = lanes.at(p, base);
@@ -107,8 +110,14 @@ __device__ __forceinline__ Division divide(const PagedParams& p, const ManyArgs&
         n = wave_total(n) * p.hkv;
       }
       // all alike, in rounds; unequal, in equal work and the longest at the least
-      const float fixed = kFixedNs[small] + (k < most ? kCutNs[small] : 0.f), span = (float)min(k, most) * kKeyNs[small] + fixed;
-      const float est = 0.5f * (ceilf(n * per_unit - 1e-3f) * span + fmaxf((load * kKeyNs[small] + n * fixed) * per_unit, span));
+      constexpr float head = D == 128 ? 1.f : 0.7f;
+      float join = 0.f;
+      if (k < most) {
+        const float parts = ceilf((float)most * __builtin_amdgcn_rcpf((float)k) - 1e-3f), second = parts > kManyFan ? ceilf(parts / kManyFan) : 0.f;
+        join = kCutNs + (second > 0.f ? 2.f : 1.f) * kLevelNs + (fminf(parts, kManyFan) + second) * (rows * D * kPartNs);
+      }
+      const float key = kKeyNs[small] * head, fixed = kFixedNs + join, span = (float)min(k, most) * key + fixed;
+      const float est = 0.5f * (ceilf(n * per_unit - 1e-3f) * span + fmaxf((load * key + n * fixed) * per_unit, span));
       if (est < best) { best = est; d.rows = rows; d.keys = k; }
     }
   }
@@ -133,7 +142,7 @@ __device__ __forceinline__ bool find_span(const PagedParams& p, const Division& 
       out.u.b = base + l;
       out.u.start = __builtin_amdgcn_readlane(s.start, l); out.u.n = __builtin_amdgcn_readlane(s.n, l);
       out.u.rows = __builtin_amdgcn_readlane(s.rows, l); out.u.kv = __builtin_amdgcn_readlane(s.kv, l);
-      const int np = __builtin_amdgcn_readlane(parts, l), nt = (out.u.rows + d.rows - 1) >> (d.rows == 64 ? 6 : 8);
+      const int np = __builtin_amdgcn_readlane(parts, l), nt = tiles_of(Seq{0, 0, out.u.rows, 0, 0}, d.rows);
       out.u.hk = at / (np * nt);
       const int rest = at - out.u.hk * np * nt;
       out.part = rest / nt;
@@ -322,17 +331,6 @@ __device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& 
         if (role == kLeaves) return;
         float2 s[kManyFan];
         if (has) {
-          m_all = -INFINITY;
-#pragma unroll
-          for (int k = 0; k < kManyFan; ++k) {
-            s[k] = make_float2(-INFINITY, 0.f);
-            if (k < count) s[k] = load_ml(part_buffer(first_slot + (int64_t)(first + k * stride) * PART_B), ml_at);
-            m_all = fmaxf(m_all, s[k].x);
-          }
-          const float m_ref = m_all == -INFINITY ? 0.f : m_all;
-          l_tot = 0.f;
-#pragma unroll
-          for (int i = 0; i < DBW * 4; ++i) acc[i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
           // (a part's pieces all at once, and the next one's while they are added)
           floatx4_t x[2][DBW * 4];
           auto ask = [&](int k) {
@@ -340,7 +338,17 @@ __device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& 
 #pragma unroll
             for (int i = 0; i < DBW * 4; ++i) x[k % 2][i] = load_part(buf, at + i * 1024);
           };
+#pragma unroll
+          for (int k = 0; k < kManyFan; ++k) s[k] = load_ml(part_buffer(first_slot + (int64_t)(first + min(k, count - 1) * stride) * PART_B), ml_at);
           ask(0);
+          m_all = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < kManyFan; ++k)
+            if (k < count) m_all = fmaxf(m_all, s[k].x);
+          const float m_ref = m_all == -INFINITY ? 0.f : m_all;
+          l_tot = 0.f;
+#pragma unroll
+          for (int i = 0; i < DBW * 4; ++i) acc[i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int k = 0; k < kManyFan; ++k) {
             if (k + 1 < kManyFan) ask(k + 1);
@@ -374,11 +382,11 @@ __device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& 
 // BOTH: row tiles of 64 too; with every unit of the chip holding one workgroup, which goes on from span to span.
 template <class E, int D, bool BOTH>
 __global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void paged_many_kernel(const PagedParams p, const ManyArgs a) {
-  constexpr int BYTES = BOTH && ManyCfg<D, 4>::SMEM_B > ManyCfg<D, 1>::SMEM_B ? ManyCfg<D, 4>::SMEM_B : ManyCfg<D, 1>::SMEM_B;
+  constexpr int BYTES = BOTH ? std::max({ManyCfg<D, 1>::SMEM_B, ManyCfg<D, 2>::SMEM_B, ManyCfg<D, 4>::SMEM_B}) : ManyCfg<D, 1>::SMEM_B;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[BYTES];
   __shared__ ManyShared sh;
   const Lanes lanes(p);
-  const Division d = divide<BOTH>(p, a, lanes);
+  const Division d = divide<BOTH, D>(p, a, lanes);
   // neighbours share an XCD and its L2 where they read the same keys
   const int per = (d.all + 7) / 8, xcd = blockIdx.x & 7;
   bool again = false;
@@ -389,7 +397,10 @@ __global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void pag
     if (again) __syncthreads();   // the span before is done with LDS
     again = true;
     if (!BOTH || d.rows == 256) many_span<E, D, 1>(p, sp, d.keys, smem, sh);
-    else if constexpr (BOTH) many_span<E, D, 4>(p, sp, d.keys, smem, sh);
+    else if constexpr (BOTH) {
+      if (d.rows == 128) many_span<E, D, 2>(p, sp, d.keys, smem, sh);
+      else many_span<E, D, 4>(p, sp, d.keys, smem, sh);
+    }
   }
 }
 
