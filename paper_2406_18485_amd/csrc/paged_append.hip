@@ -98,8 +98,8 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(const Appe
     if (is_q) lane.forward(p.row, wq, pa, pb);
     else if (is_k) lane.forward(p.row, wk, pa, pb);
     if (lane.holds) {
-      *reinterpret_cast<uint4*>(dst + lane.a) = pa;
-      *reinterpret_cast<uint4*>(dst + lane.b) = pb;
+      store_streaming(dst + lane.a, pa);
+      store_streaming(dst + lane.b, pb);
     }
   }
 }

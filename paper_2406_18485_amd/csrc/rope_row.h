@@ -17,7 +17,7 @@ constexpr int kRopeVec = std::is_same<E, float>::value ? 4 : 8;  // elements in 
 
 // 16 bytes that are written once and not read again by this kernel: past the caches' lines in use.  (A prompt of 4096 tokens, 64 heads
 // of 128, 30.4 -> 23.6 us; the 1M-token shard's rows, forward and backward, 61.6 -> 57.7; 8000 tokens of 10 heads of 64, which caches
-// would hold, 25.4 -> 24.1.)
+// would hold, 25.4 -> 24.1; 16384 tokens of 32 + 2 x 8 heads of 128 appended 89 -> 63, 64 single tokens the same.)
 typedef uint32_t rope_u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void store_streaming(void* p, uint4 v) {
   const rope_u32x4 x = {v.x, v.y, v.z, v.w};
