@@ -343,7 +343,8 @@ typedef struct loong_paged_desc {
   int32_t n_kv_heads;
   int32_t head_dim;       /* 64 or 128 */
   int32_t dtype;          /* LOONG_BF16 | LOONG_FP16 */
-  int32_t n_pages, page_size, max_pages;   /* pages in the cache; slots of a page; pages a row of page_table has */
+  int32_t n_pages, page_size, max_pages;   /* pages in the cache; slots of a page; pages a row of page_table has
+                             (max_pages * page_size at most 2^30) */
   int32_t rot_dim;        /* append: as in loong_rope_desc */
   float   eps;            /* append: as in loong_rope_desc */
   int32_t causal;         /* attention: new token i of n sees keys 0 .. kv_len - n + i; 0: all kv_len (another rank's

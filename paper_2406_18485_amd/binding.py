@@ -186,6 +186,29 @@ def _in(x, dtype, dev, name):
     return x.data_ptr()
 
 
+def _flat(x, dtype, dev, name, least):
+    """_in of numbers that lie one behind the other, at least so many."""
+    if x is None or type(x) is int:
+        return x
+    if x.dtype is dtype and x.get_device() == dev and x.numel() >= least and x.is_contiguous():
+        return x.data_ptr()
+    if x.numel() < least or not x.is_contiguous():
+        raise ValueError(f"{name} holds {x.numel()} numbers{'' if x.is_contiguous() else ', not contiguous'}; {least} are read")
+    return _in(x, dtype, dev, name)
+
+
+def _table(x, dtype, dev, desc):
+    """_in of a page table whose rows lie desc.table_stride apart."""
+    if x is None or type(x) is int:
+        return x
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 2 or shape[0] < desc.n_seqs or shape[1] < desc.max_pages:
+        raise ValueError(f"page_table is {tuple(shape)}; {desc.n_seqs} rows of {desc.max_pages} are read")
+    if strides[1] != 1 and shape[1] > 1 or strides[0] != desc.table_stride and shape[0] > 1:
+        raise ValueError(f"page_table has strides {strides}, the descriptor says {desc.table_stride} and 1")
+    return _in(x, dtype, dev, "page_table")
+
+
 def _workspace_bytes(x, n_bytes):
     if n_bytes is not None:
         return n_bytes
@@ -406,8 +429,8 @@ def qk_rope_fwd(desc: RopeDesc, q, k, q_weight, k_weight, inv_freq, positions, q
     """loong_qk_rope_fwd; weights, positions (and what of q, k is not there) may be None."""
     dev, t, f32, i32 = _on(desc.dtype)
     _check(lib.loong_qk_rope_fwd(
-        C.byref(desc), _in(q, t, dev, "q"), _in(k, t, dev, "k"), _in(q_weight, f32, dev, "q_weight"), _in(k_weight, f32, dev, "k_weight"),
-        _in(inv_freq, f32, dev, "inv_freq"), _in(positions, i32, dev, "positions"), _in(q_out, t, dev, "q_out"), _in(k_out, t, dev, "k_out"),
+        C.byref(desc), _in(q, t, dev, "q"), _in(k, t, dev, "k"), _flat(q_weight, f32, dev, "q_weight", desc.head_dim), _flat(k_weight, f32, dev, "k_weight", desc.head_dim),
+        _flat(inv_freq, f32, dev, "inv_freq", desc.rot_dim // 2), _flat(positions, i32, dev, "positions", desc.batch * desc.len), _in(q_out, t, dev, "q_out"), _in(k_out, t, dev, "k_out"),
         _stream(stream)))
 
 
@@ -422,10 +445,10 @@ def qk_rope_bwd(desc: RopeDesc, q, k, q_weight, k_weight, inv_freq, positions, d
     """loong_qk_rope_bwd; `workspace` as in attn_step_bwd."""
     dev, t, f32, i32 = _on(desc.dtype)
     _check(lib.loong_qk_rope_bwd(
-        C.byref(desc), _in(q, t, dev, "q"), _in(k, t, dev, "k"), _in(q_weight, f32, dev, "q_weight"), _in(k_weight, f32, dev, "k_weight"),
-        _in(inv_freq, f32, dev, "inv_freq"), _in(positions, i32, dev, "positions"), _in(d_q_out, f32, dev, "d_q_out"),
-        _in(d_k_out, f32, dev, "d_k_out"), _in(dq, t, dev, "dq"), _in(dk, t, dev, "dk"), _in(dq_weight, f32, dev, "dq_weight"),
-        _in(dk_weight, f32, dev, "dk_weight"), _in(workspace, None, dev, "workspace"), _workspace_bytes(workspace, workspace_bytes),
+        C.byref(desc), _in(q, t, dev, "q"), _in(k, t, dev, "k"), _flat(q_weight, f32, dev, "q_weight", desc.head_dim), _flat(k_weight, f32, dev, "k_weight", desc.head_dim),
+        _flat(inv_freq, f32, dev, "inv_freq", desc.rot_dim // 2), _flat(positions, i32, dev, "positions", desc.batch * desc.len), _in(d_q_out, f32, dev, "d_q_out"),
+        _in(d_k_out, f32, dev, "d_k_out"), _in(dq, t, dev, "dq"), _in(dk, t, dev, "dk"), _flat(dq_weight, f32, dev, "dq_weight", desc.head_dim),
+        _flat(dk_weight, f32, dev, "dk_weight", desc.head_dim), _in(workspace, None, dev, "workspace"), _workspace_bytes(workspace, workspace_bytes),
         _stream(stream)))
 
 
@@ -453,9 +476,10 @@ def paged_append(desc: PagedDesc, q, k, v, q_weight, k_weight, inv_freq, positio
     """loong_paged_append; weights and positions may be None, q and q_out together."""
     dev, t, f32, i32 = _on(desc.dtype)
     _check(lib.loong_paged_append(
-        C.byref(desc), _in(q, t, dev, "q"), _in(k, t, dev, "k"), _in(v, t, dev, "v"), _in(q_weight, f32, dev, "q_weight"),
-        _in(k_weight, f32, dev, "k_weight"), _in(inv_freq, f32, dev, "inv_freq"), _in(positions, i32, dev, "positions"),
-        _in(seq_start, i32, dev, "seq_start"), _in(kv_len, i32, dev, "kv_len"), _in(page_table, i32, dev, "page_table"),
+        C.byref(desc), _in(q, t, dev, "q"), _in(k, t, dev, "k"), _in(v, t, dev, "v"), _flat(q_weight, f32, dev, "q_weight", desc.head_dim),
+        _flat(k_weight, f32, dev, "k_weight", desc.head_dim), _flat(inv_freq, f32, dev, "inv_freq", desc.rot_dim // 2),
+        _flat(positions, i32, dev, "positions", desc.n_tokens), _flat(seq_start, i32, dev, "seq_start", desc.n_seqs + 1),
+        _flat(kv_len, i32, dev, "kv_len", desc.n_seqs), _table(page_table, i32, dev, desc),
         _in(q_out, t, dev, "q_out"), _in(k_cache, t, dev, "k_cache"), _in(v_cache, t, dev, "v_cache"), _stream(stream)))
 
 
@@ -472,6 +496,6 @@ def paged_attn(desc: PagedDesc, q, k_cache, v_cache, seq_start, kv_len, page_tab
     dev, t, f32, i32 = _on(desc.dtype)
     _check(lib.loong_paged_attn(
         C.byref(desc), _in(q, t, dev, "q"), _in(k_cache, t, dev, "k_cache"), _in(v_cache, t, dev, "v_cache"),
-        _in(seq_start, i32, dev, "seq_start"), _in(kv_len, i32, dev, "kv_len"), _in(page_table, i32, dev, "page_table"),
-        _in(out, f32, dev, "out"), _in(o, t, dev, "o"), _in(lse, f32, dev, "lse"), _in(workspace, None, dev, "workspace"),
+        _flat(seq_start, i32, dev, "seq_start", desc.n_seqs + 1), _flat(kv_len, i32, dev, "kv_len", desc.n_seqs), _table(page_table, i32, dev, desc),
+        _in(out, f32, dev, "out"), _in(o, t, dev, "o"), _flat(lse, f32, dev, "lse", desc.n_tokens * desc.n_q_heads), _in(workspace, None, dev, "workspace"),
         _workspace_bytes(workspace, workspace_bytes), _stream(stream)))

@@ -26,6 +26,7 @@ int check_paged(const loong_paged_desc* d, int flags) {
   if (d->head_dim != 64 && d->head_dim != 128) return fail(LOONG_E_UNSUPPORTED, "a paged cache takes head_dim 64 or 128, got %d", d->head_dim);
   if (d->flags & ~flags) return fail(LOONG_E_UNSUPPORTED, "flags %d: this call takes %d", d->flags, flags);
   if (d->page_size > (1 << 24)) return fail(LOONG_E_UNSUPPORTED, "page_size %d is above 2^24", d->page_size);
+  if ((int64_t)d->max_pages * d->page_size > (1 << 30)) return fail(LOONG_E_UNSUPPORTED, "more than 2^30 keys in a row of the page table");
   if (d->n_seqs > (1 << 20)) return fail(LOONG_E_UNSUPPORTED, "more than 2^20 sequences");
   if ((int64_t)d->n_tokens * d->n_q_heads > (1 << 30)) return fail(LOONG_E_UNSUPPORTED, "more than 2^30 query rows");
   const struct { const char* name; const int64_t* s; int n; } strides[] = {

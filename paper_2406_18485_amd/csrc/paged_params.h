@@ -32,11 +32,8 @@ struct PagedPlan {
   int64_t workgroups, slots;
   int slot_floats;
 };
-// keys that a sequence has pages for (kv_len is an int32)
-inline int64_t cached_keys(const loong_paged_desc& d) {
-  const int64_t n = (int64_t)d.max_pages * d.page_size;
-  return n < 0x7fffffff ? n : 0x7fffffff;
-}
+// keys that a sequence has pages for (2^30 at the most)
+inline int64_t cached_keys(const loong_paged_desc& d) { return (int64_t)d.max_pages * d.page_size; }
 PagedPlan plan_paged_few(const loong_paged_desc& d, int cus);
 PagedPlan plan_paged_many(const loong_paged_desc& d, int cus);
 void launch_paged_few(const PagedParams& p, const loong_paged_desc& d, unsigned grid, void* stream);

@@ -171,6 +171,68 @@ def test_many_sequences():
     Case([1] * 70 + [90] + [3] * 9, rng.integers(90, 120, 80).tolist(), hq=2, hkv=2, d=64, seed=4).run().check()
 
 
+def test_shares_that_end_inside_units():
+    """More grains than workgroups, lengths that are no multiples of a share; some sequences too short to be cut."""
+    rng = np.random.default_rng(1)
+    kv = rng.integers(700, 1600, 40).tolist() + rng.integers(1, 500, 30).tolist()
+    c = Case([1] * 70, kv, hq=16, hkv=8, d=64, seed=20).run().check()
+    first = c.out.clone()
+    c.reset()
+    c.run()
+    assert torch.equal(c.out, first)
+
+
+def reference_on_gpu(c):
+    """Out, lse and attention of |v| in 64 bits, a head at a time (the sizes below are too long for the oracle)."""
+    out, size = (torch.full((c.tokens, c.hq, c.d), float("nan"), dtype=torch.float64, device=DEV) for _ in range(2))
+    lse = torch.full((c.tokens, c.hq), float("nan"), dtype=torch.float64, device=DEV)
+    for b, (n, m) in enumerate(zip(c.new, c.kv)):
+        at = slice(c.starts[b], c.starts[b] + n)
+        pages = c.table[b, :-(-m // c.page)].long()
+        for h in range(c.hq):
+            keys, vals = (x[pages, h // (c.hq // c.hkv)].reshape(-1, c.d)[:m].double() for x in (c.k_cache, c.v_cache))
+            s = c.q[at, h].double() @ keys.T * c.scale
+            if c.causal:
+                s.masked_fill_(torch.ones(n, m, dtype=torch.bool, device=DEV).triu(m - n + 1), float("-inf"))
+            lse[at, h] = torch.logsumexp(s, -1)
+            s.sub_(lse[at, h, None]).exp_()
+            out[at, h], size[at, h] = s @ vals, s @ vals.abs()
+    return out, lse, size
+
+
+# row tiles of 64, 128 and 256 rows, whole and cut, by the lengths; tiles of 256 rows that fill the chip, at both head dimensions
+FORMS = [([300], [700], 8, 2, 128), ([200, 1], [3000, 2500], 8, 2, 128), ([1000], [6000], 8, 2, 128), ([1000], [6100], 8, 2, 64), ([260], [40000], 4, 1, 128),
+         ([40, 1, 33], [20000, 30000, 400], 4, 2, 64), ([2100], [2500], 32, 8, 128), ([1500, 700, 1], [1500, 3333, 900], 32, 4, 64), ([777], [5000], 96, 1, 64)]
+
+
+@pytest.mark.parametrize("new,kv,hq,hkv,d", FORMS)
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16])
+def test_long_chunks_in_every_form(new, kv, hq, hkv, d, dtype):
+    c = Case(new, kv, dtype=dtype, hq=hq, hkv=hkv, d=d, page=48, seed=21).run()
+    out, lse, size = reference_on_gpu(c)
+    u, small = U[dtype]
+    dot = c.scale * 1.01 * (c.q.double().norm(dim=-1).max() * c.k_cache.double().nan_to_num().norm(dim=-1).max()).item()
+    noise = (2 * max(kv) + 64) * E + 2 * d * E * dot
+    off = (u + noise) * size + small * max(kv) * c.v_cache.double().nan_to_num().abs().max().item()
+    assert ((c.out.double() - out).abs() <= off).all()
+    assert ((c.o.double() - out).abs() <= off + u * (out.abs() + off) + small).all()
+    assert ((c.lse.double() - lse).abs() <= noise + 2 * E * lse.abs()).all()
+    first = c.out.clone()
+    c.reset()
+    c.run()
+    assert torch.equal(c.out, first)
+    # an infinity among the last values: the last token alone sees it
+    b = 0
+    page, slot = int(c.table_np[b, (kv[b] - 1) // c.page]), (kv[b] - 1) % c.page
+    c.v_cache[page, :, slot, 1] = float("inf")
+    c.reset()
+    c.run()
+    last = c.starts[b + 1] - 1
+    assert (c.out[last, :, 1] == float("inf")).all()
+    c.out[last, :, 1] = first[last, :, 1]
+    assert torch.equal(c.out, first)
+
+
 def test_large_scores_move_the_maximum():
     for new in ([1], [100]):
         Case(new, [700], sigma=6.0, seed=5).run().check()

@@ -62,7 +62,8 @@ def _refused(call, code):
     (dict(max_new=-1), P.E_SHAPE), (dict(n_q_heads=0), P.E_SHAPE), (dict(n_kv_heads=0), P.E_SHAPE), (dict(n_kv_heads=3), P.E_UNSUPPORTED),
     (dict(head_dim=96), P.E_UNSUPPORTED), (dict(page_size=0), P.E_SHAPE), (dict(page_size=(1 << 24) + 1), P.E_UNSUPPORTED),
     (dict(n_pages=-1), P.E_SHAPE), (dict(max_pages=-1), P.E_SHAPE), (dict(flags=2), P.E_UNSUPPORTED), (dict(n_tokens=1 << 28), P.E_UNSUPPORTED),
-    (dict(n_seqs=(1 << 20) + 1), P.E_UNSUPPORTED), (dict(q_stride=(1024, 132)), P.E_ALIGN), (dict(kv_stride=(-8, 128)), P.E_SHAPE),
+    (dict(n_seqs=(1 << 20) + 1), P.E_UNSUPPORTED), (dict(max_pages=1 << 27), P.E_UNSUPPORTED),
+    (dict(cache_stride=(4096, 2048, 1 << 31)), P.E_UNSUPPORTED), (dict(q_stride=(1024, 132)), P.E_ALIGN), (dict(kv_stride=(-8, 128)), P.E_SHAPE),
     (dict(cache_stride=(4096, 2048, 4)), P.E_ALIGN), (dict(o_stride=(1 << 41, 128)), P.E_SHAPE), (dict(table_stride=-1), P.E_SHAPE)])
 def test_descriptors_that_are_refused(kw, code):
     d = _desc(**kw)
@@ -116,3 +117,12 @@ def test_workspace_only_where_a_context_can_be_shared():
 def test_tensors_that_no_kernel_may_read_are_refused():
     with pytest.raises(ValueError, match="page_table is on cpu"):
         _attn(_desc(), page_table=torch.zeros(3, 32, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("name,x,text", [
+    ("seq_start", torch.zeros(3, dtype=torch.int32), "4 are read"), ("kv_len", torch.zeros(6, dtype=torch.int32)[::2], "not contiguous"),
+    ("page_table", torch.zeros(2, 32, dtype=torch.int32), "3 rows of 32 are read"),
+    ("page_table", torch.zeros(3, 40, dtype=torch.int32), "strides"), ("lse", torch.zeros(20, 7), "160 are read")])
+def test_tables_that_are_too_short_are_refused(name, x, text):
+    with pytest.raises(ValueError, match=text):
+        _attn(_desc(), **{name: x})

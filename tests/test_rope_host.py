@@ -124,6 +124,16 @@ def test_tensors_that_no_kernel_may_read_are_refused():
         _fwd(_desc(), q=x)
 
 
+@pytest.mark.parametrize("kw,text", [
+    (dict(wq=torch.ones(64)), "128 are read"), (dict(f=torch.ones(63)), "64 are read"), (dict(pos=torch.zeros(2, 63, dtype=torch.int32)), "128 are read"),
+    (dict(pos=torch.zeros(64, 2, dtype=torch.int32).T), "not contiguous")])
+def test_weights_and_positions_that_are_too_short_are_refused(kw, text):
+    with pytest.raises(ValueError, match=text):
+        _fwd(_desc(), **kw)
+    with pytest.raises(ValueError, match=text):
+        _bwd(_desc(), **kw)
+
+
 def test_nothing_to_do_is_no_error():
     _fwd(_desc(len=0))
     _fwd(_desc(batch=0))
