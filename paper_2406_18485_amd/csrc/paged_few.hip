@@ -1,17 +1,23 @@
 // Paged attention of few rows: up to 32 query rows of a kv head (one new token, or a few drafted ones).
 //
-// Bound by HBM, 2 e head_dim bytes a key: a matrix instruction for 32 rows is spent on as few as there are and still takes a
-// quarter of the time that its keys take to arrive.  Every wave has tiles of keys and LDS of its own and waits for nobody;
+// Bound by HBM, 2 e head_dim bytes a key: the 16 matrix instructions of 32 keys, for 32 rows however few there are, keep a SIMD for 512
+// clocks, and a unit's share of the memory's rate needs 1000 for their 16 KB.  Every wave has tiles of keys and LDS of its own and waits for nobody;
 // while one of its K and V tiles is used the other is on its way: 8 waves a unit keep 64 to 128 KB in flight.
 //
 // Division.  All keys of all units (a sequence's rows of one kv head) are put in one line and cut into equal shares, one for every
 // workgroup of a launch that the chip holds at once: however unequal the lengths, all end together.  A workgroup works on
 // the units of its share one after the other.  Lengths are in device memory: every wave works out the line from them (a lane a
-// sequence, or a run of them).  Units of up to kShort grains are not cut: they are whole in the share that they begin in.  (48 sequences of
-// 1000 to 8192 keys, 8 kv heads, against spans of one length that the hardware deals out: FIG_BATCH us; two of 262144, one head: FIG_LONG.)
+// sequence, or a run of them).  Units of up to kShort grains are not cut: they are whole in the share that they begin in, and where there
+// are workgroups enough every unit begins with a share of its own.  (48 sequences of 1000 to 8192 keys, 8 kv heads: 148.5 us with spans of
+// one length that the hardware deals out, 138.8 with shares; one sequence of 4000 keys, 8 heads, shares that straddle units 16.2, apart 12.3.)
 //
-// A cut unit's shares are added up by the last to arrive (split_exchange.h), kFewFan at a time, so that a context spread over
-// the whole chip is not read by one workgroup.  (All 512 shares of a unit by one: 115 us for the two contexts above.)
+// A cut unit's shares are added up by the last to arrive (split_exchange.h), kFewFan at a time, so that the results of a context spread
+// over the whole chip are not read by one workgroup.  (Two contexts of 262144 keys, one kv head: 127 us with 512 parts added up by
+// one workgroup, 77 sixteen at a time.  A further level costs 5 us: 16000 keys of 8 heads, 62 parts, 22.5 us in two, 20.3 in one.)
+//
+// 48 sequences, 708 MB of keys and values: 137 us, 5.2 TB/s (64 of 4000 keys 5.6).  The shortest call, one sequence of up to 32 keys, takes 7.4 us, a launch
+// alone 2.3: the rest is the chain of loads lengths -> page numbers -> keys, a microsecond each, and the sums over waves; an
+// exchange adds 3.5.
 #include <hip/hip_runtime.h>
 
 #include "paged_body.h"

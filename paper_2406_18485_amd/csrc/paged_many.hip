@@ -5,11 +5,15 @@
 // token, the group's q heads of each) are cut into tiles of 256 / KS.
 //
 // Division.  A unit (sequence, kv head, row tile) may be cut into spans of keys, which are added up by the last of them to arrive
-// (split_exchange.h), kManyFan at a time.  Whole units of 256 rows use the matrix cores best (KS = 1: 1030 to 1090 TFLOP/s over long contexts,
-// KS = 4 640 to 710), but where they are fewer than the chip's units either they are cut, which costs an exchange of 128 KB a span, or the
-// row tiles are made smaller.  Which is faster goes by the lengths, which are in device memory: every wave works out, for both and for
-// a few lengths of a span, how many spans there would be and about how long they would take, and all take the best.  (1000 tokens, 8
-// heads on 2, KS = 1 / KS = 4: over 1000 keys 27 / 22 us, 6000 53 / 54, 16000 90 / 110, 64000 271 / 365.)
+// (split_exchange.h), kManyFan at a time.  Tiles of 256 rows use the matrix cores best (KS = 1: 1030 to 1090 TFLOP/s over long contexts,
+// KS = 2 840, KS = 4 640 to 710), but where there are fewer of them than units of the chip either they are cut, which costs an exchange of
+// 128 KB a span, or the tiles are made smaller.  Which is faster goes by the lengths, which are in device memory: every wave works out,
+// for the three tiles and for a few lengths of a span, how many spans there would be and about how long they would take, and all take
+// the best.  (1000 tokens, 8 heads on 2, KS = 1 / 2 / 4 in us: over 1000 keys 27 / 22 / 22, 6000 53 / 55 / 54, 16000 90 / 100 / 110, 64000
+// 271 / 312 / 365; with the choice 20, 49, 93, 272.  Beside eight decoding sequences, 6000 keys: 59 / 52 / 64, with it 52.5.)
+//
+// 2048 tokens over 32768 keys, 32 heads on 8: 995 to 1050 us by the box's clock (1020 to 1080 TFLOP/s, the matrix cores busy for 51 % of
+// their cycles); what keeps them waiting is the vector work of the softmax, as in the forward step.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -30,6 +34,7 @@ constexpr float kKeyNs[3] = {31.5f, 18.5f, 12.f}, kFixedNs = 9500.f, kCutNs = 15
 
 struct ManyArgs {
   int cus;
+  int hold;     // workgroups that the chip holds at once: cus, or two for each
   int units;    // that there can be, at the most
 };
 
@@ -68,7 +73,7 @@ template <bool BOTH, int D>
 __device__ __forceinline__ Division divide(const PagedParams& p, const ManyArgs& a, const Lanes& lanes) {
   Division d{256, 0, 0};
   float best = INFINITY;
-  const float cus = (float)a.cus, per_unit = __builtin_amdgcn_rcpf(cus);
+  const float hold = (float)a.hold, per_place = __builtin_amdgcn_rcpf(hold), slower = hold * __builtin_amdgcn_rcpf((float)a.cus);
   int most = 0;
   for (int base = 0; base < p.n_seqs; base += 64) {
     const Seq s = lanes.at(p, base);
@@ -88,8 +93,8 @@ __device__ __forceinline__ Division divide(const PagedParams& p, const ManyArgs&
     load = wave_total(load) * p.hkv;
     units = wave_total(units) * p.hkv;
     if (units == 0.f || units > (float)a.units) return Division{256, 1, 0};   // (more than there can be: seq_start decreases somewhere)
-    // not cut; cut so that every unit of the chip has a span of the longest; cut into equal work
-    const float even = load * per_unit, fit = floorf(cus * __builtin_amdgcn_rcpf(units) + 1e-3f);
+    // not cut; cut so that there is a span of the longest for all that the chip holds; cut into equal work
+    const float even = load * per_place, fit = floorf(hold * __builtin_amdgcn_rcpf(units) + 1e-3f);
 #pragma unroll 1
     for (int c = 0; c < 3; ++c) {
       if (c == 1 && fit < 2.f) continue;
@@ -98,7 +103,7 @@ __device__ __forceinline__ Division divide(const PagedParams& p, const ManyArgs&
       k = max(k, kManyLeast);
       if (c > 0 && k >= most) continue;
       // (what bounds the number of spans, and their slots: cutting adds at most kManyMore a unit of the chip)
-      if (k < most && load > (float)k * (kManyMore * 0.999f) * cus) continue;
+      if (k < most && load > (float)k * (kManyMore * 0.999f) * (float)a.cus) continue;
       float n = units;
       if (k < most) {
         const float inv = __builtin_amdgcn_rcpf((float)k);
@@ -116,8 +121,8 @@ __device__ __forceinline__ Division divide(const PagedParams& p, const ManyArgs&
         const float parts = ceilf((float)most * __builtin_amdgcn_rcpf((float)k) - 1e-3f), second = parts > kManyFan ? ceilf(parts / kManyFan) : 0.f;
         join = kCutNs + (second > 0.f ? 2.f : 1.f) * kLevelNs + (fminf(parts, kManyFan) + second) * (rows * D * kPartNs);
       }
-      const float key = kKeyNs[small] * head, fixed = kFixedNs + join, span = (float)min(k, most) * key + fixed;
-      const float est = 0.5f * (ceilf(n * per_unit - 1e-3f) * span + fmaxf((load * key + n * fixed) * per_unit, span));
+      const float key = kKeyNs[small] * head * slower, fixed = kFixedNs + join, span = (float)min(k, most) * key + fixed;
+      const float est = 0.5f * (ceilf(n * per_place - 1e-3f) * span + fmaxf((load * key + n * fixed) * per_place, span));
       if (est < best) { best = est; d.rows = rows; d.keys = k; }
     }
   }
@@ -379,7 +384,8 @@ __device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& 
   if (ksp == 0 && hh == 0) p.lse[(int64_t)token * p.hq + head] = lse_of(m_all, l_tot);
 }
 
-// BOTH: row tiles of 64 too; with every unit of the chip holding one workgroup, which goes on from span to span.
+// BOTH: row tiles of 128 and 64 too; with every unit of the chip holding one workgroup, which goes on from span to span.
+// (Else, at head_dim 64, two workgroups a unit fit: 8000 tokens over 30000 keys 2125 -> 1996 us.)
 template <class E, int D, bool BOTH>
 __global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void paged_many_kernel(const PagedParams p, const ManyArgs a) {
   constexpr int BYTES = BOTH ? std::max({ManyCfg<D, 1>::SMEM_B, ManyCfg<D, 2>::SMEM_B, ManyCfg<D, 4>::SMEM_B}) : ManyCfg<D, 1>::SMEM_B;
@@ -441,7 +447,7 @@ PagedPlan plan_paged_many(const loong_paged_desc& d, int cus) {
 void launch_paged_many(const PagedParams& p, const loong_paged_desc& d, int cus, unsigned grid, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool both = !rows_fill(d, cus);
-  const ManyArgs a{cus, (int)most_units(d, both ? 64 : 256)};
+  const ManyArgs a{cus, d.head_dim == 64 && !both ? 2 * cus : cus, (int)most_units(d, both ? 64 : 256)};
   if (d.dtype == LOONG_BF16) {
     if (d.head_dim == 128) launch<Bf16, 128>(p, both, a, grid, st);
     else launch<Bf16, 64>(p, both, a, grid, st);

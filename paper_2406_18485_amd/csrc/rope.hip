@@ -1,8 +1,10 @@
 // Norms of query and key heads with the position rotation, and their gradient: what lies between a projection and the
 // first attention step, and between the last backward step and the projection's gradient.
 //
-// A group of lanes takes a token and walks over (a share of) its heads: the cosines and sines, some 40 instructions a pair,
-// are formed once for all of them.  Bound by HBM: forward 2 e bytes per element (e: its size), backward 2 e + 4.
+// A group of lanes takes a token and walks over (a share of) its heads: the cosines and sines, some ten instructions a pair, five of
+// them in 64 bits, are formed once for all of them.  Bound by HBM: forward 2 e bytes per element (e: its size), backward 2 e + 4.  Inputs that
+// are in no cache: a prompt of 4096 tokens of 64 heads of 128, 134 MB, 23 us (5.7 TB/s; a plain elementwise pass reaches 5.3 at that
+// size); the 1M-token shard's rows, 32768 tokens of 5 heads, forward 84 MB 17 us, backward 168 MB 35 us and 4 for the weights.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -86,8 +88,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeParams
 }
 
 // dx = r (w g) - x r^3 mean(w g x), g the gradient rotated back; a weight's gradient is the sum of g x r over all rows.
-// A workgroup takes heads of q or of k and walks over token blocks, the next row's loads in flight while one is computed; its
-// sums go to the workspace, and the kernel behind this one adds them up in order.
+// A workgroup takes heads of q or of k and walks over token blocks, the next row's loads in flight while one is computed (48 us instead
+// of the 35 above without, and with heads of both in a workgroup); its sums go to the workspace, and the kernel behind this one adds them up in order.
 template <class E, bool INTER>
 __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeParams p) {
   typedef typename StorageOf<E>::type T;

@@ -69,7 +69,7 @@ struct RopeLane {
   // The angle p f is reduced in 64 bits, in turns: at a position of a million its whole turns leave 32 bits too few.  The
   // reduced one, rounded to 32 bits (1.9e-7 of a radian at most), goes to the hardware's sine and cosine, which take turns and are
   // 1.2e-7 off at most, 3.4e-8 rms (measured over four million angles; the library's 5e-8 and 1.5e-8 at four times the
-  // instructions: rows of 8 + 2 heads of 64, forward and backward, 34 -> 27 us).
+  // instructions: the 1M-token shard's rows, forward and backward, 60.4 -> 57.6 us, prompts appended in half 10.4 -> 8.9).
   __device__ __forceinline__ void turn(const RopeRow& r, int s, int64_t pos) {
     const double p = (double)pos * 0.15915494309189535;   // 1 / (2 pi)
 #pragma unroll
