@@ -385,7 +385,9 @@ __device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& 
 }
 
 // BOTH: row tiles of 128 and 64 too; with every unit of the chip holding one workgroup, which goes on from span to span.
-// (Else, at head_dim 64, two workgroups a unit fit: 8000 tokens over 30000 keys 2125 -> 1996 us.)
+// Else, at head_dim 64, two workgroups a unit fit, in 128 registers and with 68 bytes of scratch memory, of which the loop over
+// tiles reads one value: 8000 tokens over 30000 keys, 32 heads on 8, 2125 -> 1996 us.  (The other side: 2500 tokens' own prompt, 32 heads of own keys, 320
+// tiles for 256 units, 60 -> 80 us, as the units that hold two end last; over 8000 keys, where tiles are cut, 249 -> 227.)
 template <class E, int D, bool BOTH>
 __global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void paged_many_kernel(const PagedParams p, const ManyArgs a) {
   constexpr int BYTES = BOTH ? std::max({ManyCfg<D, 1>::SMEM_B, ManyCfg<D, 2>::SMEM_B, ManyCfg<D, 4>::SMEM_B}) : ManyCfg<D, 1>::SMEM_B;
@@ -410,8 +412,16 @@ __global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void pag
   }
 }
 
-// Are there row tiles of 256 for every unit of the chip?
-bool rows_fill(const loong_paged_desc& d, int cus) { return (int64_t)d.n_tokens * d.n_q_heads >= (int64_t)256 * cus; }
+// Are row tiles of 256 alone better?  They are where every unit of the chip has one.  At head_dim 64, where two workgroups share a unit that takes
+// tiles of 256 only, they are with fewer rows too if the contexts are long, as far as the page table says: it has room for 2^18 scores
+// a unit.  (32 heads on 8, 1500 tokens: over 1500 / 8000 / 30000 keys 39 / 164 / 580 us with all three tiles, 31 / 137 / 487 so; 700 tokens, over
+// 1500 / 2500 / 4000 / 30000 keys 28.7 / 40.8 / 54.3 / 301 and 32.6 / 40.4 / 50.0 / 224; three prompts of 500 20.5 and 27.  A table with much more
+// room than keys costs those few us; below 64 rows a unit it would cost half as much again, 400 tokens over 1500 keys 22.5 and 35.)
+bool rows_fill(const loong_paged_desc& d, int cus) {
+  const int64_t rows = (int64_t)d.n_tokens * d.n_q_heads;
+  if (rows >= (int64_t)256 * cus) return true;
+  return d.head_dim == 64 && rows >= (int64_t)64 * cus && cached_keys(d) >= ((int64_t)cus << 18) / rows;
+}
 int64_t most_units(const loong_paged_desc& d, int rows) {
   const int64_t group = d.n_q_heads / d.n_kv_heads;
   return ((d.n_seqs < d.n_tokens ? d.n_seqs : d.n_tokens) + d.n_tokens * group / rows) * d.n_kv_heads;

@@ -202,7 +202,9 @@ def reference_on_gpu(c):
 
 # row tiles of 64, 128 and 256 rows, whole and cut, by the lengths; tiles of 256 rows that fill the chip, at both head dimensions
 FORMS = [([300], [700], 8, 2, 128), ([200, 1], [3000, 2500], 8, 2, 128), ([1000], [6000], 8, 2, 128), ([1000], [6100], 8, 2, 64), ([260], [40000], 4, 1, 128),
-         ([40, 1, 33], [20000, 30000, 400], 4, 2, 64), ([2100], [2500], 32, 8, 128), ([1500, 700, 1], [1500, 3333, 900], 32, 4, 64), ([777], [5000], 96, 1, 64)]
+         ([40, 1, 33], [20000, 30000, 400], 4, 2, 64), ([2100], [2500], 32, 8, 128), ([1500, 700, 1], [1500, 3333, 900], 32, 4, 64), ([777], [5000], 96, 1, 64),
+         # fewer rows than fill the chip with tiles of 256, head_dim 64, tables with room for many keys and for few
+         ([700], [4800], 32, 8, 64), ([520, 9, 1], [2500, 4500, 100], 32, 4, 64), ([1, 0, 1100, 33], [9000, 0, 1100, 2000], 16, 16, 64), ([700], [2000], 32, 8, 64)]
 
 
 @pytest.mark.parametrize("new,kv,hq,hkv,d", FORMS)
