@@ -11,7 +11,7 @@ def test_nothing_in_scratch_memory(kernels):  # noqa: F811
     for name, k in _named(kernels, "paged_few|paged_append|rope_fwd|rope_bwd|rope_weight").items():
         assert k[".private_segment_fixed_size"] == 0, name
     for name, k in _named(kernels, "paged_many").items():
-        # (head_dim 64, two workgroups a unit, 128 registers: some of what a span keeps outside its loop)
+        # (head_dim 64, two workgroups a unit, 128 registers: what a span keeps, one value of it read in the loop over tiles)
         most = 80 if "ELi64ELb0E" in name else 0
         assert k[".private_segment_fixed_size"] <= most, (name, k[".private_segment_fixed_size"])
 
