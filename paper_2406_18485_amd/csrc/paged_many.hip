@@ -19,29 +19,14 @@
 #include <algorithm>
 
 #include "paged_body.h"
+#include "paged_division.h"
 
 namespace loong {
 namespace {
 
 constexpr int kManyWaves = 8;
-constexpr int kManyFan = 4;            // parts that are added up at a time
 constexpr int kManyLevels = 6;         // 4^6 parts are more than a unit has
-constexpr int kManyLeast = 256;        // keys of a span of a cut unit, at the least
-constexpr int kManyMore = 2;           // spans that cutting may add, per unit of the chip
-// What a span takes, in ns: per key at head_dim 128 (KS = 1, 2, 4; 0.7 of it at 64) and whatever it has; if its unit is cut, every level of
-// adding parts up takes its waits, and every part that is added what one workgroup needs to read it (50 bytes a ns).
-constexpr float kKeyNs[3] = {31.5f, 18.5f, 12.f}, kFixedNs = 9500.f, kCutNs = 1500.f, kLevelNs = 1500.f, kPartNs = 0.08f;
 
-struct ManyArgs {
-  int cus;
-  int hold;     // workgroups that the chip holds at once: cus, or two for each
-  int units;    // that there can be, at the most
-};
-
-// How all the work is divided: rows of a tile, keys of a span, spans.
-struct Division {
-  int rows, keys, all;
-};
 struct ManySpan {
   Unit u;
   int part;
@@ -65,74 +50,50 @@ struct Lanes {
     return s;
   }
 };
-__device__ __forceinline__ int tiles_of(const Seq& s, int rows) { return (s.rows + rows - 1) >> (rows == 64 ? 6 : rows == 128 ? 7 : 8); }
-__device__ __forceinline__ int parts_of(const Seq& s, int keys) { return s.paged <= keys ? 1 : (int)((uint32_t)(s.paged - 1) / (uint32_t)keys) + 1; }
+__device__ __forceinline__ int tiles_of(const Seq& s, int rows) { return row_tiles(s.rows, rows); }
+__device__ __forceinline__ int parts_of(const Seq& s, int keys) { return key_parts(s.paged, keys); }
 
-// (Estimates in floats: an integer division is some 40 instructions, and all this is in front of the first load of a key.)
-template <bool BOTH, int D>
-__device__ __forceinline__ Division divide(const PagedParams& p, const ManyArgs& a, const Lanes& lanes) {
-  Division d{256, 0, 0};
-  float best = INFINITY;
-  const float hold = (float)a.hold, per_place = __builtin_amdgcn_rcpf(hold), slower = hold * __builtin_amdgcn_rcpf((float)a.cus);
-  int most = 0;
-  for (int base = 0; base < p.n_seqs; base += 64) {
-    const Seq s = lanes.at(p, base);
-    most = max(most, s.rows ? s.paged : 0);
+// What the division asks of all sequences, by a wave.
+struct WaveSums {
+  const PagedParams& p;
+  const Lanes& lanes;
+  static __device__ __forceinline__ float rcp(float x) { return __builtin_amdgcn_rcpf(x); }
+  __device__ __forceinline__ int longest() const {
+    int most = 0;
+    for (int base = 0; base < p.n_seqs; base += 64) {
+      const Seq s = lanes.at(p, base);
+      most = max(most, s.rows ? s.paged : 0);
+    }
+    return wave_most(most);
   }
-  most = wave_most(most);
-#pragma unroll
-  for (int small = 0; small < (BOTH ? 3 : 1); ++small) {
-    const int rows = 256 >> small;
-    float load = 0.f, units = 0.f;
+  __device__ __forceinline__ void tiles(int rows, float& load, float& units) const {
+    load = units = 0.f;
     for (int base = 0; base < p.n_seqs; base += 64) {
       const Seq s = lanes.at(p, base);
       const float t = (float)tiles_of(s, rows);
       load += t * (float)s.paged;
       units += t;
     }
-    load = wave_total(load) * p.hkv;
-    units = wave_total(units) * p.hkv;
-    if (units == 0.f || units > (float)a.units) return Division{256, 1, 0};   // (more than there can be: seq_start decreases somewhere)
-    // not cut; cut so that there is a span of the longest for all that the chip holds; cut into equal work
-    const float even = load * per_place, fit = floorf(hold * __builtin_amdgcn_rcpf(units) + 1e-3f);
-#pragma unroll 1
-    for (int c = 0; c < 3; ++c) {
-      if (c == 1 && fit < 2.f) continue;
-      const float want = c == 0 ? (float)most : c == 1 ? (float)most * __builtin_amdgcn_rcpf(fit) + 1.f : even;
-      int k = want < 2e9f ? ((int)want + 63) / 64 * 64 : most;
-      k = max(k, kManyLeast);
-      if (c > 0 && k >= most) continue;
-      // (what bounds the number of spans, and their slots: cutting adds at most kManyMore a unit of the chip)
-      if (k < most && load > (float)k * (kManyMore * 0.999f) * (float)a.cus) continue;
-      float n = units;
-      if (k < most) {
-        const float inv = __builtin_amdgcn_rcpf((float)k);
-        n = 0.f;
-        for (int base = 0; base < p.n_seqs; base += 64) {
-          const Seq s = lanes.at(p, base);
-          n += (float)tiles_of(s, rows) * fmaxf(ceilf((float)s.paged * inv - 1e-4f), 1.f);
-        }
-        n = wave_total(n) * p.hkv;
-      }
-      // all alike, in rounds; unequal, in equal work and the longest at the least
-      constexpr float head = D == 128 ? 1.f : 0.7f;
-      float join = 0.f;
-      if (k < most) {
-        const float parts = ceilf((float)most * __builtin_amdgcn_rcpf((float)k) - 1e-3f), second = parts > kManyFan ? ceilf(parts / kManyFan) : 0.f;
-        join = kCutNs + (second > 0.f ? 2.f : 1.f) * kLevelNs + (fminf(parts, kManyFan) + second) * (rows * D * kPartNs);
-      }
-      const float key = kKeyNs[small] * head * slower, fixed = kFixedNs + join, span = (float)min(k, most) * key + fixed;
-      const float est = 0.5f * (ceilf(n * per_place - 1e-3f) * span + fmaxf((load * key + n * fixed) * per_place, span));
-      if (est < best) { best = est; d.rows = rows; d.keys = k; }
+    load = wave_total(load);
+    units = wave_total(units);
+  }
+  __device__ __forceinline__ float spans(int rows, float inv) const {
+    float n = 0.f;
+    for (int base = 0; base < p.n_seqs; base += 64) {
+      const Seq s = lanes.at(p, base);
+      n += (float)tiles_of(s, rows) * fmaxf(ceilf((float)s.paged * inv - 1e-4f), 1.f);
     }
+    return wave_total(n);
   }
-  for (int base = 0; base < p.n_seqs; base += 64) {
-    const Seq s = lanes.at(p, base);
-    d.all += tiles_of(s, d.rows) * parts_of(s, d.keys);
+  __device__ __forceinline__ int all(const Division& d) const {
+    int n = 0;
+    for (int base = 0; base < p.n_seqs && !d.none; base += 64) {
+      const Seq s = lanes.at(p, base);
+      n += tiles_of(s, d.rows) * parts_of(s, d.keys);
+    }
+    return wave_total(n) * p.hkv;
   }
-  d.all = wave_total(d.all) * p.hkv;
-  return d;
-}
+};
 
 __device__ __forceinline__ bool find_span(const PagedParams& p, const Division& d, const Lanes& lanes, int item, ManySpan& out) {
   int before = 0, slot = 0;
@@ -394,14 +355,16 @@ __global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void pag
   __shared__ __attribute__((aligned(1024))) unsigned char smem[BYTES];
   __shared__ ManyShared sh;
   const Lanes lanes(p);
-  const Division d = divide<BOTH, D>(p, a, lanes);
+  const WaveSums sums{p, lanes};
+  const Division d = choose_division<BOTH, D>(sums, p.hkv, a);
+  const int all = sums.all(d);   // spans
   // neighbours share an XCD and its L2 where they read the same keys
-  const int per = (d.all + 7) / 8, xcd = blockIdx.x & 7;
+  const int per = (all + 7) / 8, xcd = blockIdx.x & 7;
   bool again = false;
   for (int idx = blockIdx.x >> 3; idx < per; idx += gridDim.x >> 3) {
     ManySpan sp;
     const int item = xcd * per + idx;
-    if (item >= d.all || !find_span(p, d, lanes, item, sp)) break;
+    if (item >= all || !find_span(p, d, lanes, item, sp)) break;
     if (again) __syncthreads();   // the span before is done with LDS
     again = true;
     if (!BOTH || d.rows == 256) many_span<E, D, 1>(p, sp, d.keys, smem, sh);
@@ -410,21 +373,6 @@ __global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void pag
       else many_span<E, D, 4>(p, sp, d.keys, smem, sh);
     }
   }
-}
-
-// Are row tiles of 256 alone better?  They are where every unit of the chip has one.  At head_dim 64, where two workgroups share a unit that takes
-// tiles of 256 only, they are with fewer rows too if the contexts are long, as far as the page table says: it has room for 2^18 scores
-// a unit.  (32 heads on 8, 1500 tokens: over 1500 / 8000 / 30000 keys 39 / 164 / 580 us with all three tiles, 31 / 137 / 487 so; 700 tokens, over
-// 1500 / 2500 / 4000 / 30000 keys 28.7 / 40.8 / 54.3 / 301 and 32.6 / 40.4 / 50.0 / 224; three prompts of 500 20.5 and 27.  A table with much more
-// room than keys costs those few us; below 64 rows a unit it would cost half as much again, 400 tokens over 1500 keys 22.5 and 35.)
-bool rows_fill(const loong_paged_desc& d, int cus) {
-  const int64_t rows = (int64_t)d.n_tokens * d.n_q_heads;
-  if (rows >= (int64_t)256 * cus) return true;
-  return d.head_dim == 64 && rows >= (int64_t)64 * cus && cached_keys(d) >= ((int64_t)cus << 18) / rows;
-}
-int64_t most_units(const loong_paged_desc& d, int rows) {
-  const int64_t group = d.n_q_heads / d.n_kv_heads;
-  return ((d.n_seqs < d.n_tokens ? d.n_seqs : d.n_tokens) + d.n_tokens * group / rows) * d.n_kv_heads;
 }
 
 template <class E, int D>
@@ -436,28 +384,12 @@ void launch(const PagedParams& p, bool both, const ManyArgs& a, unsigned grid, h
 
 }  // namespace
 
-// Where row tiles of 256 fill the chip the hardware deals the spans out, else as many workgroups as it holds take them in turn.
-// Spans of cut units are longer than load / (kManyMore cus) (0.999 of it: the sum is a float), so that there are at most kManyMore cus of
-// them and a remainder a unit, and at most as many units are cut.
-PagedPlan plan_paged_many(const loong_paged_desc& d, int cus) {
-  PagedPlan pl{};
-  const bool both = !rows_fill(d, cus);
-  const int64_t units = most_units(d, both ? 64 : 256);
-  const int64_t keys = cached_keys(d), parts = keys <= kManyLeast ? 1 : (keys + kManyLeast - 1) / kManyLeast;
-  const int64_t more = (int64_t)(kManyMore * cus * 1.01) + 8;
-  int64_t spans = units + more;
-  if (units * parts < spans) spans = units * parts;
-  pl.workgroups = both && spans > cus ? cus : spans;
-  pl.workgroups = (pl.workgroups + 7) / 8 * 8;
-  pl.slots = parts == 1 ? 0 : 2 * more < spans ? 2 * more : spans;
-  pl.slot_floats = 256 * (d.head_dim + 4);
-  return pl;
-}
+PagedPlan plan_paged_many(const loong_paged_desc& d, int cus) { return plan_many(d, cus); }
 
 void launch_paged_many(const PagedParams& p, const loong_paged_desc& d, int cus, unsigned grid, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool both = !rows_fill(d, cus);
-  const ManyArgs a{cus, d.head_dim == 64 && !both ? 2 * cus : cus, (int)most_units(d, both ? 64 : 256)};
+  const ManyArgs a = many_args(d, cus);
   if (d.dtype == LOONG_BF16) {
     if (d.head_dim == 128) launch<Bf16, 128>(p, both, a, grid, st);
     else launch<Bf16, 64>(p, both, a, grid, st);
