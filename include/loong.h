@@ -284,8 +284,8 @@ LOONG_API int loong_reduce_replicas(int64_t heads, int32_t rep, int64_t elems_pe
 
 typedef struct loong_rope_desc {
   int32_t batch;
-  int32_t n_q_heads;      /* 0: there is no q (its pointers may be NULL) */
-  int32_t n_kv_heads;     /* 0: there is no k */
+  int32_t n_q_heads;      /* 0: there is no q (its pointers may be NULL); 2^20 at most */
+  int32_t n_kv_heads;     /* 0: there is no k; 2^20 at most */
   int32_t head_dim;       /* a multiple of 16, at most 256 */
   int32_t rot_dim;        /* a multiple of 16, 0 .. head_dim */
   int32_t len;            /* tokens per batch element */
@@ -339,7 +339,7 @@ typedef struct loong_paged_desc {
   int32_t n_tokens;       /* rows of q, k, v, out, lse */
   int32_t max_new;        /* attention: no sequence has more new tokens; rows past that are left as they are.  (1 when decoding;
                              n_tokens if nothing better is known) */
-  int32_t n_q_heads;      /* q head h reads kv head h / (n_q_heads / n_kv_heads) */
+  int32_t n_q_heads;      /* q head h reads kv head h / (n_q_heads / n_kv_heads); 2^20 at most */
   int32_t n_kv_heads;
   int32_t head_dim;       /* 64 or 128 */
   int32_t dtype;          /* LOONG_BF16 | LOONG_FP16 */

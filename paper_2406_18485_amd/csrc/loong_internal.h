@@ -124,6 +124,9 @@ int64_t bwd_steps_that_fit_bf16(const loong_step_desc& d, const StepGeom& g);
 int launch_delta(const loong_step_desc& d, const void* o, const void* d_o, float* delta, void* head, void* stream);
 int launch_clear_head(void* head, void* stream);
 
+// Heads that the calls on either side of the step take: sums of their numbers stay far inside 32 bits.
+constexpr int kMaxHeads = 1 << 20;
+
 // Validate a descriptor of the paged cache (no device access); `flags`: those the call takes.
 int check_paged(const loong_paged_desc* d, int flags);
 }  // namespace loong

@@ -25,6 +25,7 @@ int check_paged(const loong_paged_desc* d, int flags) {
                 d->n_seqs, d->n_tokens, d->max_new, d->n_q_heads, d->n_kv_heads, d->n_pages, d->page_size, d->max_pages);
   if (d->n_q_heads % d->n_kv_heads != 0)
     return fail(LOONG_E_UNSUPPORTED, "n_q_heads %d is not a multiple of n_kv_heads %d", d->n_q_heads, d->n_kv_heads);
+  if (d->n_q_heads > kMaxHeads) return fail(LOONG_E_UNSUPPORTED, "%d query heads: %d at most", d->n_q_heads, kMaxHeads);
   if (d->head_dim != 64 && d->head_dim != 128) return fail(LOONG_E_UNSUPPORTED, "a paged cache takes head_dim 64 or 128, got %d", d->head_dim);
   if (d->flags & ~flags) return fail(LOONG_E_UNSUPPORTED, "flags %d: this call takes %d", d->flags, flags);
   if (d->page_size > (1 << 24)) return fail(LOONG_E_UNSUPPORTED, "page_size %d is above 2^24", d->page_size);

@@ -228,6 +228,8 @@ int check_rope(const loong_rope_desc* d) {
     return fail(LOONG_E_DTYPE, "dtype %d is none of LOONG_BF16, LOONG_FP32, LOONG_FP16", d->dtype);
   if (d->batch < 0 || d->len < 0 || d->n_q_heads < 0 || d->n_kv_heads < 0 || (int64_t)d->n_q_heads + d->n_kv_heads < 1)
     return fail(LOONG_E_SHAPE, "negative size or no heads (batch %d, len %d, heads %d/%d)", d->batch, d->len, d->n_q_heads, d->n_kv_heads);
+  if (d->n_q_heads > kMaxHeads || d->n_kv_heads > kMaxHeads)
+    return fail(LOONG_E_UNSUPPORTED, "heads %d/%d: %d of either at most", d->n_q_heads, d->n_kv_heads, kMaxHeads);
   if (d->head_dim < 16 || d->head_dim > 256 || d->head_dim % 16 != 0)
     return fail(LOONG_E_UNSUPPORTED, "head_dim %d is not a multiple of 16 up to 256", d->head_dim);
   if (d->rot_dim < 0 || d->rot_dim > d->head_dim || d->rot_dim % 16 != 0)
