@@ -312,7 +312,8 @@ LOONG_API int loong_qk_rope_fwd(const loong_rope_desc* desc, const void* q, cons
  * Where a weight's gradient is wanted, `workspace` is device memory of the caller's, 16-byte aligned, of
  * loong_qk_rope_workspace_bytes(desc) bytes; it may hold anything on entry; calls that share one must be ordered on one
  * stream.  Without LOONG_QK_NORM there are no weights: their gradients' pointers must be NULL.
- * Errors of both calls: LOONG_E_NULL, LOONG_E_SHAPE, LOONG_E_UNSUPPORTED, LOONG_E_ALIGN (tensors 16-byte aligned, strides multiples of
+ * Errors of both calls: LOONG_E_NULL, LOONG_E_SHAPE (also where rows of a result lie on each other: a stride below head_dim in a direction
+ * of more than one; inputs may be broadcast, but not q, k of the gradient, whose strides dq, dk have), LOONG_E_UNSUPPORTED, LOONG_E_ALIGN (tensors 16-byte aligned, strides multiples of
  * 16 bytes), LOONG_E_DTYPE.
  */
 LOONG_API int loong_qk_rope_bwd(const loong_rope_desc* desc, const void* q, const void* k, const float* q_weight, const float* k_weight,
@@ -355,7 +356,8 @@ typedef struct loong_paged_desc {
   int64_t q_stride[2];    /* token, head strides (elements) of q */
   int64_t kv_stride[2];   /* append: of the new k and v */
   int64_t o_stride[2];    /* append: of q_out; attention: of out and o */
-  int64_t cache_stride[3];/* page, head, slot strides of k_cache and v_cache */
+  int64_t cache_stride[3];/* page, head, slot strides of k_cache and v_cache.  (What a call writes must not lie on itself: no stride of it
+                             below head_dim in a direction of more than one.  Inputs may be broadcast.) */
 } loong_paged_desc;
 
 /*

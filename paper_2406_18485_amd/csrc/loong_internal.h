@@ -127,6 +127,9 @@ int launch_clear_head(void* head, void* stream);
 // Heads that the calls on either side of the step take: sums of their numbers stay far inside 32 bits.
 constexpr int kMaxHeads = 1 << 20;
 
+// May a result have this stride in a direction of `n`?  (Rows on each other would be written by several workgroups at once.)
+inline bool apart(int64_t stride, int64_t n, int head_dim) { return n <= 1 || stride >= head_dim; }
+
 // Validate a descriptor of the paged cache (no device access); `flags`: those the call takes.
 int check_paged(const loong_paged_desc* d, int flags);
 }  // namespace loong

@@ -138,6 +138,11 @@ int loong_paged_append(const loong_paged_desc* desc, const void* q, const void* 
   for (const void* x : {(const void*)positions, (const void*)seq_start, (const void*)kv_len, (const void*)page_table})
     if (reinterpret_cast<uintptr_t>(x) & 3) return fail(LOONG_E_ALIGN, "loong_paged_append: table or inv_freq not 4-byte aligned");
   if (d.n_tokens == 0 || d.n_seqs == 0) return LOONG_OK;
+  const int64_t cached[3] = {d.n_pages, d.n_kv_heads, d.page_size}, rows[2] = {d.n_tokens, d.n_q_heads};
+  for (int i = 0; i < 3; ++i)
+    if (!apart(d.cache_stride[i], cached[i], d.head_dim)) return fail(LOONG_E_SHAPE, "cache_stride[%d] = %lld: slots lie on each other", i, (long long)d.cache_stride[i]);
+  for (int i = 0; i < 2 && q; ++i)
+    if (!apart(d.o_stride[i], rows[i], d.head_dim)) return fail(LOONG_E_SHAPE, "o_stride[%d] = %lld: rows of a result lie on each other", i, (long long)d.o_stride[i]);
   AppendParams p{};
   p.row = make_rope_row(d.head_dim, d.rot_dim, 8, norm, d.eps, inv_freq);
   p.q = (const uint16_t*)q; p.k = (const uint16_t*)k; p.v = (const uint16_t*)v;

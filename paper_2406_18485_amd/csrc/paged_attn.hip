@@ -60,6 +60,9 @@ int loong_paged_attn(const loong_paged_desc* desc, const void* q, const void* k_
   for (const void* x : {(const void*)seq_start, (const void*)kv_len, (const void*)page_table, (const void*)lse})
     if (reinterpret_cast<uintptr_t>(x) & 3) return fail(LOONG_E_ALIGN, "loong_paged_attn: table or lse not 4-byte aligned");
   if (d.n_tokens == 0 || d.n_seqs == 0 || d.max_new == 0) return LOONG_OK;
+  const int64_t rows[2] = {d.n_tokens, d.n_q_heads};
+  for (int i = 0; i < 2; ++i)
+    if (!apart(d.o_stride[i], rows[i], d.head_dim)) return fail(LOONG_E_SHAPE, "o_stride[%d] = %lld: rows of a result lie on each other", i, (long long)d.o_stride[i]);
   if (d.n_pages == 0) return fail(LOONG_E_SHAPE, "loong_paged_attn: a cache without pages");
   DeviceFacts dev;
   if (int rc = device_facts(&dev)) return rc;

@@ -254,6 +254,15 @@ int check_rope(const loong_rope_desc* d) {
   return LOONG_OK;
 }
 
+// the rows of a result of q's or k's heads, by its strides
+int check_rope_result(const loong_rope_desc& d, const char* name, const int64_t* stride, int heads) {
+  const int64_t n[3] = {d.batch, heads, d.len};
+  if (d.batch == 0 || d.len == 0 || heads == 0) return LOONG_OK;
+  for (int i = 0; i < 3; ++i)
+    if (!apart(stride[i], n[i], d.head_dim)) return fail(LOONG_E_SHAPE, "%s[%d] = %lld: rows of a result lie on each other", name, i, (long long)stride[i]);
+  return LOONG_OK;
+}
+
 // Forward: token blocks x shares of the heads; a group of lanes takes so many heads that the launch still has some `kFwdPerCu`
 // workgroups for every unit.  Backward: a workgroup has heads of q or of k and walks over every so-manieth token block; there are as
 // many of either as gives all of them equal work and every unit about `kBwdPerCu`, what its registers have room for.
@@ -347,6 +356,8 @@ int loong_qk_rope_fwd(const loong_rope_desc* desc, const void* q, const void* k,
   const float* w[2] = {q_weight, k_weight};
   const void *qs[4] = {q, q_out}, *ks[4] = {k, k_out};
   if (int rc = check_rope_tensors(*desc, "loong_qk_rope_fwd", inv_freq, positions, w, qs, ks, 2)) return rc;
+  if (int rc = check_rope_result(*desc, "q_out_stride", desc->q_out_stride, desc->n_q_heads)) return rc;
+  if (int rc = check_rope_result(*desc, "k_out_stride", desc->k_out_stride, desc->n_kv_heads)) return rc;
   const RopePlan pl = plan_rope(*desc, row_of(*desc, nullptr), planning_cus());
   if (pl.token_blocks == 0) return LOONG_OK;
   if (pl.shares > 65535 || !launch_fits(pl.token_blocks * pl.shares, kRopeThreads)) return fail(LOONG_E_UNSUPPORTED, "loong_qk_rope_fwd: grid too large");
@@ -378,6 +389,8 @@ int loong_qk_rope_bwd(const loong_rope_desc* desc, const void* q, const void* k,
   const float* w[2] = {q_weight, k_weight};
   const void *qs[4] = {q, d_q_out, dq}, *ks[4] = {k, d_k_out, dk};
   if (int rc = check_rope_tensors(*desc, "loong_qk_rope_bwd", inv_freq, positions, w, qs, ks, 3)) return rc;
+  if (int rc = check_rope_result(*desc, "q_stride (of dq)", desc->q_stride, desc->n_q_heads)) return rc;
+  if (int rc = check_rope_result(*desc, "k_stride (of dk)", desc->k_stride, desc->n_kv_heads)) return rc;
   const bool norm = (desc->flags & LOONG_QK_NORM) != 0, sums = dq_weight || dk_weight;
   if (sums && !norm) return fail(LOONG_E_UNSUPPORTED, "loong_qk_rope_bwd: gradients of weights without LOONG_QK_NORM");
   if ((dq_weight && desc->n_q_heads == 0) || (dk_weight && desc->n_kv_heads == 0))
