@@ -1,0 +1,121 @@
+"""Paged calls on the GPU where a context has more parts than are added up at a time, and where a group of lanes appends many heads.
+Bounds as in the tests of short calls (test_gpu_vs_oracle_paged)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2406_18485_amd as P
+from gpu_harness import DEV
+from oracle import paged_oracle as po
+from oracle import rope_oracle as ro
+from test_gpu_vs_oracle_paged import E, TORCH, U, Case, f64, reference_on_gpu
+
+pytestmark = pytest.mark.gpu
+
+PART, FAN = 256, 64     # keys of a part of a context that has the chip to itself, up to 131072 of them; parts that are added up at a time
+
+
+def check(c):
+    out, lse, size = reference_on_gpu(c)
+    blind = torch.isneginf(lse)       # rows that see no key (the reference's softmax of nothing is NaN)
+    assert torch.equal(blind, torch.isneginf(c.lse)) and (c.out[blind] == 0).all() and (c.o[blind] == 0).all()
+    out[blind], size[blind], lse[blind] = 0, 0, float("-inf")
+    u, small = U[c.dtype]
+    dot = c.scale * 1.01 * (c.q.double().norm(dim=-1).max() * c.k_cache.double().nan_to_num().norm(dim=-1).max()).item()
+    noise = (2 * max(c.kv) + 64) * E + 2 * c.d * E * dot
+    off = (u + noise) * size + small * max(c.kv) * c.v_cache.double().nan_to_num().abs().max().item()
+    assert ((c.out.double() - out).abs() <= off).all()
+    assert ((c.o.double() - out).abs() <= off + u * (out.abs() + off) + small).all()
+    assert ((c.lse.double() - lse).abs()[~blind] <= (noise + 2 * E * lse.abs())[~blind]).all()
+    assert (c.ws[:P.WORKSPACE_HEAD] == 0).all()       # every counter is back at zero
+    first = c.out.clone(), c.lse.clone()
+    c.reset()
+    c.run()
+    assert torch.equal(c.out, first[0]) and torch.equal(c.lse, first[1])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq", [1, 8, 32])
+@pytest.mark.parametrize("kv", [PART * (FAN - 1) + 1, PART * FAN, PART * FAN + 1, PART * (FAN + 1), 2 * PART * FAN, 2 * PART * FAN + 1, 4 * PART * FAN - 3])
+def test_parts_around_what_is_added_up_at_a_time(kv, hq, d):
+    """63, 64 (one level), 65 (a lone last part), 66, 128, 129 and 256 parts."""
+    check(Case([1], [kv], hq=hq, hkv=1, d=d, page=64, clean=True, seed=hq + d).run())
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_contexts_of_unequal_lengths(d, dtype):
+    # apart from each other: every unit begins with a share of its own
+    check(Case([1, 1, 2], [70001, 30000, 17000], dtype=dtype, hq=8, hkv=1, d=d, page=48, clean=True, seed=1).run())
+    # 2559 grains of 64 keys in shares of 5: the second unit begins inside one
+    check(Case([1, 1], [1001 * 64, 1558 * 64], dtype=dtype, hq=4, hkv=1, d=d, page=256, clean=True, seed=2).run())
+    # and with sequences that are not cut between them
+    check(Case([1, 2, 1, 1, 3, 1], [20000, 100, 41000, 512, 1, 33333], dtype=dtype, hq=8, hkv=2, d=d, page=16, clean=True, seed=3).run())
+
+
+def test_rows_that_see_less_than_the_longest():
+    """Drafted tokens at the border of a part, and more new tokens than are asked for."""
+    check(Case([4], [PART * (FAN + 1) + 2], hq=4, hkv=1, d=128, page=64, clean=True, seed=4).run())
+    c = Case([6], [PART * FAN + 4], hq=4, hkv=1, d=64, page=64, max_new=2, clean=True, seed=5).run()
+    full = Case([6], [PART * FAN + 4], hq=4, hkv=1, d=64, page=64, clean=True, seed=5)
+    out, lse, size = reference_on_gpu(full)
+    noise = (2 * full.kv[0] + 64) * E
+    assert ((c.out.double() - out).abs()[:2] <= (U[P.BF16][0] + noise + 1e-5) * size[:2]).all() and (c.out[2:] == 7).all()
+    assert ((c.lse.double() - lse).abs()[:2] <= 1e-4).all() and (c.ws[:P.WORKSPACE_HEAD] == 0).all()
+
+
+def test_replays_between_one_level_and_two():
+    c = Case([1, 1], [70000, 40000], hq=4, hkv=1, d=64, page=64, clean=True, seed=6)
+    lengths = [[70000, 40000], [PART * FAN, PART * FAN], [PART * FAN + 1, 5], [300, 40000], [1, 0], [70000, 39999]]
+    want = []
+    for kv in lengths:
+        c.kv_len.copy_(torch.tensor(kv, dtype=torch.int32))
+        c.reset()
+        c.run()
+        want.append((c.out.clone(), c.lse.clone()))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.run()
+    for _ in range(2):
+        for kv, (out, lse) in zip(lengths, want):
+            c.kv_len.copy_(torch.tensor(kv, dtype=torch.int32))
+            c.out.fill_(3.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
+            assert (c.ws[:P.WORKSPACE_HEAD] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,d,rot,norm,inter", [(P.BF16, 128, 128, True, False), (P.FP16, 64, 32, False, True)])
+def test_append_of_many_tokens(dtype, d, rot, norm, inter):
+    """Several heads a group of lanes: of q, of k and of v."""
+    new, kv, hq, hkv = [7001, 1, 2300, 4099], [9000, 50, 2300, 4100], 9, 3
+    c = Case(new, kv, dtype=dtype, d=d, hq=hq, hkv=hkv, page=48, before=1, behind=2, seed=7)
+    lanes = d // 16
+    assert -(-c.tokens // (256 // lanes)) * (hq + 2 * hkv) >= 2 * 4 * torch.cuda.get_device_properties(0).multi_processor_count
+    gen = torch.Generator().manual_seed(8)
+    k, v = (torch.randn(c.tokens, hkv, d, generator=gen).to(TORCH[dtype]).to(DEV) for _ in range(2))
+    wq, wk = (1 + 0.3 * torch.randn(d, generator=gen).to(DEV) if norm else None for _ in range(2))
+    f = (10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)).float().to(DEV)
+    before = f64(c.k_cache), f64(c.v_cache)
+    q_out = torch.full_like(c.q, 7.0)
+    desc = P.make_paged_desc(n_seqs=len(kv), n_tokens=c.tokens, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, dtype=dtype, n_pages=c.n_pages, page_size=48,
+                             max_pages=c.width, table_stride=c.width + 2, rot_dim=rot, eps=1e-5,
+                             flags=(P.QK_NORM if norm else 0) | (P.ROPE_INTERLEAVED if inter else 0))
+    P.paged_append(desc, c.q, k, v, wq, wk, f, None, c.seq_start, c.kv_len, c.table, q_out, c.k_cache, c.v_cache)
+    w = lambda x: None if x is None else f64(x)
+    kc, vc = po.append(*before, f64(k), f64(v), w(wk), 1e-5, None, f64(f), inter, norm, c.starts, kv, c.table_np)
+    got_k, got_v = f64(c.k_cache), f64(c.v_cache)
+    assert np.array_equal(got_v, vc, equal_nan=True) and np.array_equal(np.isnan(got_k), np.isnan(kc))
+    u, small = U[dtype]
+
+    def close(got, want, x, weight):
+        size = 1.5 * (np.sqrt(d) * np.abs(f64(weight)).max() if norm else np.sqrt((f64(x) ** 2).sum(-1)).max())
+        assert (np.abs(got - want) <= 32 * E * size + u * (np.abs(want) + 32 * E * size) + small).all()
+    ok = ~np.isnan(kc)
+    close(got_k[ok], kc[ok], k, wk)
+    lo, hi = c.starts[0], c.starts[-1]
+    slots = np.concatenate([np.arange(m - n, m) for n, m in zip(new, kv)])
+    close(f64(q_out)[lo:hi], ro.rope_forward(f64(c.q)[lo:hi], w(wq), 1e-5, slots[:, None], f64(f), inter, norm), c.q[lo:hi], wq)
+    assert (q_out[:lo] == 7).all() and (q_out[hi:] == 7).all()

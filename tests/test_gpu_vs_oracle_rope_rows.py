@@ -1,0 +1,67 @@
+"""Norm and rotation on the GPU where a group of lanes has many rows, and where a row's numbers are at the ends of their range.
+Bounds as in the tests of single rows (test_gpu_vs_oracle_rope)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2406_18485_amd as P
+from gpu_harness import DEV
+from oracle import rope_oracle as ro
+from test_gpu_vs_oracle_rope import E, TORCH, U, Case, f64
+
+pytestmark = pytest.mark.gpu
+
+
+def rows_per_unit(c):
+    """Rows of lane groups (tokens of a workgroup x heads) for every unit of the chip."""
+    lanes = 1 << (c.d // (8 if c.dtype == P.FP32 else 16) - 1).bit_length()
+    blocks = -(-c.b * c.n // (256 // lanes))
+    return blocks * (c.hq + c.hkv) / torch.cuda.get_device_properties(0).multi_processor_count
+
+
+# heads that a group's share does not divide, of which it has some of q and some of k; a last block of few tokens
+MANY = [(P.BF16, 3, 2333, 9, 3, 128, 128, False), (P.FP16, 2, 3499, 11, 2, 128, 64, True), (P.FP32, 2, 1501, 9, 3, 128, 128, False),
+        (P.FP32, 1, 1301, 16, 1, 256, 32, True), (P.BF16, 1, 12001, 13, 5, 64, 64, True)]
+
+
+@pytest.mark.parametrize("dtype,b,n,hq,hkv,d,rot,inter", MANY)
+def test_groups_of_many_heads_and_blocks(dtype, b, n, hq, hkv, d, rot, inter):
+    c = Case(dtype, b, n, hq, hkv, d, rot, inter=inter, layout="tokens", where="given", seed=n)
+    assert rows_per_unit(c) > 4    # more than a row for every group, forward (4 a unit) and backward (3)
+    c.fwd()
+    c.bwd()
+    c.check_fwd()
+    c.check_bwd()
+    first = [x.clone() for x in (c.dq, c.dk, c.dwq, c.dwk)]
+    c.ws.fill_(0x7F)
+    c.bwd()
+    assert all(torch.equal(a, x) for a, x in zip(first, (c.dq, c.dk, c.dwq, c.dwk)))   # bit-reproducible
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP32])
+def test_groups_of_many_heads_in_place(dtype):
+    c = Case(dtype, 2, 3499, 9, 3, 128, 128, layout="heads", seed=1)
+    assert rows_per_unit(c) > 4
+    c.fwd()
+    q, k = c.q.clone(), c.k.clone()
+    P.qk_rope_fwd(c.desc, q, k, c.wq, c.wk, c.f, None, q, k)
+    assert torch.equal(q, c.q_out) and torch.equal(k, c.k_out)
+    # gradients over the forward's inputs
+    c.bwd()
+    want = c.dq.clone(), c.dk.clone(), c.dwq.clone(), c.dwk.clone()
+    P.qk_rope_bwd(c.desc, c.q, c.k, c.wq, c.wk, c.f, None, c.dqo, c.dko, c.q, c.k, c.dwq, c.dwk, c.ws)
+    assert all(torch.equal(a, x) for a, x in zip(want, (c.q, c.k, c.dwq, c.dwk)))
+
+
+def test_a_group_with_rows_of_one_side_alone():
+    for hq, hkv in ((11, 0), (0, 11)):
+        c = Case(P.BF16, 3, 2333, hq, hkv, 128, 128, seed=2)
+        assert rows_per_unit(c) > 4
+        if hq == 0:
+            c.q = c.q_out = c.dqo = c.dq = c.dwq = None
+        else:
+            c.k = c.k_out = c.dko = c.dk = c.dwk = None
+        c.fwd()
+        c.bwd()
+        c.check_fwd()
+        c.check_bwd()
