@@ -56,12 +56,14 @@ struct RopeLane {
   static constexpr int V = kRopeVec<E>;
   int a, b;              // element offsets of the two pieces
   bool holds;            // (of 2^lg lanes those past the row's end hold nothing)
+  bool turns;            // its pairs are rotated.  (By 0 is not the same: infinity x 0 would make a NaN of its neighbour.)
   float cs[V], sn[V];
 
   __device__ __forceinline__ RopeLane(const RopeRow& r, int s) {
     holds = s < r.pieces2;
+    turns = s < r.rot2;
     s = holds ? s : 0;
-    const bool apart = !INTER && s < r.rot2;
+    const bool apart = !INTER && turns;
     a = (apart ? s : 2 * s) * V;
     b = (apart ? s + r.rot2 : 2 * s + 1) * V;
   }
@@ -74,8 +76,8 @@ struct RopeLane {
     const double p = (double)pos * 0.15915494309189535;   // 1 / (2 pi)
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
-      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);   // (what is not rotated turns by 0)
-      if (s < r.rot2) f = *reinterpret_cast<const float4*>(r.inv_freq + s * V + i);
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (turns) f = *reinterpret_cast<const float4*>(r.inv_freq + s * V + i);
       turn_one(p, f.x, i); turn_one(p, f.y, i + 1); turn_one(p, f.z, i + 2); turn_one(p, f.w, i + 3);
     }
   }
@@ -103,16 +105,16 @@ struct RopeLane {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float u = x[first(i)], v = x[second(i)];
-      x[first(i)] = u * cs[i] - v * sn[i];
-      x[second(i)] = u * sn[i] + v * cs[i];
+      x[first(i)] = turns ? u * cs[i] - v * sn[i] : u;
+      x[second(i)] = turns ? u * sn[i] + v * cs[i] : v;
     }
   }
   __device__ __forceinline__ void rotate_back(float (&x)[2 * V]) const {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float u = x[first(i)], v = x[second(i)];
-      x[first(i)] = u * cs[i] + v * sn[i];
-      x[second(i)] = v * cs[i] - u * sn[i];
+      x[first(i)] = turns ? u * cs[i] + v * sn[i] : u;
+      x[second(i)] = turns ? v * cs[i] - u * sn[i] : v;
     }
   }
 

@@ -119,3 +119,22 @@ def test_append_of_many_tokens(dtype, d, rot, norm, inter):
     slots = np.concatenate([np.arange(m - n, m) for n, m in zip(new, kv)])
     close(f64(q_out)[lo:hi], ro.rope_forward(f64(c.q)[lo:hi], w(wq), 1e-5, slots[:, None], f64(f), inter, norm), c.q[lo:hi], wq)
     assert (q_out[:lo] == 7).all() and (q_out[hi:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("rot", [0, 32])
+def test_appended_infinities_and_nan_in_elements_that_are_not_rotated(dtype, rot, inter):
+    c = Case([5], [12], dtype=dtype, d=64, hq=4, hkv=2, seed=9)
+    k, v = torch.randn(5, 2, 64, device=DEV).to(TORCH[dtype]), torch.randn(5, 2, 64, device=DEV).to(TORCH[dtype])
+    for x in (c.q, k):
+        x[0, :, rot], x[1, :, 63], x[3, :, rot + 5] = float("inf"), float("-inf"), float("nan")
+    q_out = torch.full_like(c.q, 7.0)
+    desc = P.make_paged_desc(n_seqs=1, n_tokens=5, n_q_heads=4, n_kv_heads=2, head_dim=64, dtype=dtype, n_pages=c.n_pages, page_size=16,
+                             max_pages=c.width, table_stride=c.width + 2, rot_dim=rot, flags=P.ROPE_INTERLEAVED if inter else 0)
+    f = torch.ones(max(rot // 2, 1), device=DEV)
+    P.paged_append(desc, c.q, k, v, None, None, f, None, c.seq_start, c.kv_len, c.table, q_out, c.k_cache, c.v_cache)
+    slots = c.k_cache[int(c.table_np[0, 0]), :, 7:12].transpose(0, 1)
+    same = lambda a, b: torch.equal(a[..., rot:].nan_to_num(nan=77.0), b[..., rot:].nan_to_num(nan=77.0))
+    assert same(q_out, c.q) and same(slots, k)
+    assert torch.isfinite(q_out[..., :rot]).all() and torch.isfinite(slots[..., :rot]).all()

@@ -65,3 +65,26 @@ def test_a_group_with_rows_of_one_side_alone():
         c.bwd()
         c.check_fwd()
         c.check_bwd()
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16, P.FP32])
+@pytest.mark.parametrize("d,rot", [(64, 32), (128, 0), (80, 48), (16, 0)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_infinities_and_nan_in_elements_that_are_not_rotated(dtype, d, rot, inter):
+    """They pass as they are, and so do their neighbours."""
+    c = Case(dtype, 1, 9, 3, 1, d, rot, norm=False, inter=inter, seed=3)
+    odd = [(0, rot, float("inf")), (1, d - 1, float("-inf")), (2, rot + 3, float("nan"))]
+    for i, at, x in odd:
+        c.q[0, :, i, at] = x
+        c.dqo[0, :, i, at] = x
+    c.fwd()
+    c.bwd()
+    assert torch.equal(c.q_out[..., rot:].nan_to_num(nan=77.0), c.q[..., rot:].nan_to_num(nan=77.0))
+    assert torch.equal(c.dq[..., rot:].nan_to_num(nan=77.0), c.dqo[..., rot:].to(TORCH[dtype]).nan_to_num(nan=77.0))
+    for i, at, x in odd:
+        c.q[0, :, i, at] = 0
+        c.dqo[0, :, i, at] = 0
+    want = c.q_out.clone(), c.dq.clone()
+    c.fwd()
+    c.bwd()
+    assert torch.equal(c.q_out[..., :rot], want[0][..., :rot]) and torch.equal(c.dq[..., :rot], want[1][..., :rot])
