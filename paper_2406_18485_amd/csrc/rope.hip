@@ -87,7 +87,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeParams
   }
 }
 
-// dx = r (w g) - x r^3 mean(w g x), g the gradient rotated back; a weight's gradient is the sum of g x r over all rows.
+// dx = r (w g - x r mean(w g x r)), g the gradient rotated back; a weight's gradient is the sum of g x r over all rows.  (Every factor is
+// of a normal size that way: r^3 alone passes the largest float at rows of rms 1e-13, with an eps of 0.)
 // A workgroup takes heads of q or of k and walks over token blocks, the next row's loads in flight while one is computed (48 us instead
 // of the 35 above without, and with heads of both in a workgroup); its sums go to the workspace, and the kernel behind this one adds them up in order.
 template <class E, bool INTER>
@@ -161,11 +162,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeParams
         dot += gy[i] * w[i] * xv[i];
       }
       lane.row_sums(p.row, sq, dot);
-      const float inv = rsqrtf(sq * p.row.inv_d + p.row.eps), c = dot * p.row.inv_d * (inv * inv * inv);
+      const float inv = rsqrtf(sq * p.row.inv_d + p.row.eps), mean = dot * inv * p.row.inv_d;
 #pragma unroll
       for (int i = 0; i < 2 * V; ++i) {
-        dw[i] += gy[i] * (xv[i] * inv);
-        gy[i] = gy[i] * w[i] * inv - xv[i] * c;
+        const float hat = xv[i] * inv;
+        dw[i] += gy[i] * hat;
+        gy[i] = (gy[i] * w[i] - hat * mean) * inv;
       }
     }
     T* row = (T*)p.y[which] + cur.x;

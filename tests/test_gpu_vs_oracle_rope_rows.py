@@ -88,3 +88,26 @@ def test_infinities_and_nan_in_elements_that_are_not_rotated(dtype, d, rot, inte
     c.fwd()
     c.bwd()
     assert torch.equal(c.q_out[..., :rot], want[0][..., :rot]) and torch.equal(c.dq[..., :rot], want[1][..., :rot])
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP32])
+@pytest.mark.parametrize("size", [1e-14, 3e-16])
+def test_gradient_of_small_rows_without_eps(dtype, size):
+    """The norm's factor is some 1e14 and 1e15, its cube past the largest float; the gradient itself is not."""
+    c = Case(dtype, 1, 40, 3, 2, 64, 64, seed=4)
+    c.q.mul_(size)
+    c.k.mul_(size)
+    c.desc.eps = 0.0
+    c.fwd()
+    c.bwd()
+    for x, w, y, g, dx, dw in ((c.q, c.wq, c.q_out, c.dqo, c.dq, c.dwq), (c.k, c.wk, c.k_out, c.dko, c.dk, c.dwk)):
+        want, want_dw = ro.rope_backward(f64(x), f64(w), 0.0, c.pos[:, None], f64(c.f), f64(g), False, True)
+        gabs = c.pair_sum(np.abs(f64(g)))
+        r = 1 / np.sqrt((f64(x) ** 2).mean(-1, keepdims=True))
+        hat, habs = np.abs(f64(x)) * r, gabs * np.abs(f64(w))
+        off = 64 * E * r * (habs + hat * (habs * hat).mean(-1, keepdims=True))
+        assert (np.abs(f64(dx) - want) <= off + U[dtype][0] * (np.abs(want) + off)).all()
+        assert (np.abs(f64(dw) - want_dw) <= (x.shape[1] * 40 + 64) * E * (gabs * hat).reshape(-1, 64).sum(0)).all()
+        out = ro.rope_forward(f64(x), f64(w), 0.0, c.pos[:, None], f64(c.f), False, True)
+        off = 32 * E * c.pair_sum(np.abs(f64(w)) * hat)
+        assert (np.abs(f64(y) - out) <= off + U[dtype][0] * (np.abs(out) + off)).all()
