@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(const Appe
   if (token >= p.n_tokens || b >= p.n_seqs) return;
   const int start = max(p.seq_start[b], 0), n_new = min(p.seq_start[b + 1], p.n_tokens) - start;
   if (token < start) return;
-  const int64_t slot = (int64_t)p.kv_len[b] - n_new + (token - start);
+  const int64_t slot = (int64_t)max(p.kv_len[b], 0) - n_new + (token - start);
   int64_t at = -1;   // where the token lies in the cache (elements), or nowhere
   if (slot >= 0 && slot < (int64_t)p.max_pages * p.page_size) {
     const uint32_t idx = (uint32_t)slot / (uint32_t)p.page_size, in = (uint32_t)slot - idx * (uint32_t)p.page_size;

@@ -138,3 +138,21 @@ def test_appended_infinities_and_nan_in_elements_that_are_not_rotated(dtype, rot
     same = lambda a, b: torch.equal(a[..., rot:].nan_to_num(nan=77.0), b[..., rot:].nan_to_num(nan=77.0))
     assert same(q_out, c.q) and same(slots, k)
     assert torch.isfinite(q_out[..., :rot]).all() and torch.isfinite(slots[..., :rot]).all()
+
+
+def test_queries_of_a_sequence_whose_length_is_negative_are_rotated_as_with_none():
+    """A negative kv_len counts as 0: its new tokens lie before the first slot."""
+    c = Case([4, 3], [0, 9], hq=4, hkv=2, d=128, seed=10)
+    k, v = (torch.randn(7, 2, 128, device=DEV).to(torch.bfloat16) for _ in range(2))
+    desc = P.make_paged_desc(n_seqs=2, n_tokens=7, n_q_heads=4, n_kv_heads=2, head_dim=128, dtype=P.BF16, n_pages=c.n_pages, page_size=16,
+                             max_pages=c.width, table_stride=c.width + 2)
+    f = (10000.0 ** (-torch.arange(0, 128, 2, dtype=torch.float64) / 128)).float().to(DEV)
+    got = []
+    for kv in (0, -1, -1000, -2 ** 31):
+        c.kv_len[0] = kv
+        q_out = torch.full_like(c.q, 7.0)
+        P.paged_append(desc, c.q, k, v, None, None, f, None, c.seq_start, c.kv_len, c.table, q_out, c.k_cache, c.v_cache)
+        got.append(q_out)
+    assert all(torch.equal(x, got[0]) for x in got)
+    want = ro.rope_forward(f64(c.q)[:4], None, 0.0, np.arange(-4, 0)[:, None], f64(f), False, False)
+    assert np.abs(f64(got[0])[:4] - want).max() <= 2.0 ** -8 * np.abs(want).max() + 1e-5
