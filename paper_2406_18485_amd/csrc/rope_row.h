@@ -68,10 +68,11 @@ struct RopeLane {
     b = (apart ? s + r.rot2 : 2 * s + 1) * V;
   }
 
-  // The angle p f is reduced in 64 bits, in turns: at a position of a million its whole turns leave 32 bits too few.  The
-  // reduced one, rounded to 32 bits (1.9e-7 of a radian at most), goes to the hardware's sine and cosine, which take turns and are
-  // 1.2e-7 off at most, 3.4e-8 rms (measured over four million angles; the library's 5e-8 and 1.5e-8 at four times the
-  // instructions: the 1M-token shard's rows, forward and backward, 60.4 -> 57.6 us, prompts appended in half 10.4 -> 8.9).
+  // The angle p f is reduced in 64 bits, in turns: at a position of a million its whole turns leave 32 bits too few.
+  // For results in 16 bits the reduced one, rounded to 32 bits, goes to the hardware's sine and cosine, which take turns: 1.8e-7 off at
+  // most with that rounding (over a million angles), a thousandth of what the result's own rounding is.  (The library's, at four times the
+  // instructions: the 1M-token shard's rows, forward and backward, 57.6 -> 60.4 us, prompts appended in half 8.9 -> 10.4.)
+  // Results in 32 bits would show it.  They get the library's, and to first order what the rounding of the reduced angle left out.
   __device__ __forceinline__ void turn(const RopeRow& r, int s, int64_t pos) {
     const double p = (double)pos * 0.15915494309189535;   // 1 / (2 pi)
 #pragma unroll
@@ -83,9 +84,18 @@ struct RopeLane {
   }
   __device__ __forceinline__ void turn_one(double p, float f, int i) {
     const double turns = p * (double)f;
-    const float x = (float)(turns - __builtin_rint(turns));
-    sn[i] = __builtin_amdgcn_sinf(x);
-    cs[i] = __builtin_amdgcn_cosf(x);
+    const double part = turns - __builtin_rint(turns);
+    const float x = (float)part;
+    if constexpr (std::is_same<E, float>::value) {
+      float u, v;
+      sincospif(2.f * x, &u, &v);
+      const float left = 6.2831853f /* 2 pi */ * (float)(part - (double)x);
+      sn[i] = fmaf(left, v, u);
+      cs[i] = fmaf(-left, u, v);
+    } else {
+      sn[i] = __builtin_amdgcn_sinf(x);
+      cs[i] = __builtin_amdgcn_cosf(x);
+    }
   }
 
   // the lane's 2 V weights (ones if there are none)

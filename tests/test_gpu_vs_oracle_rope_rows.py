@@ -111,3 +111,19 @@ def test_gradient_of_small_rows_without_eps(dtype, size):
         out = ro.rope_forward(f64(x), f64(w), 0.0, c.pos[:, None], f64(c.f), False, True)
         off = 32 * E * c.pair_sum(np.abs(f64(w)) * hat)
         assert (np.abs(f64(y) - out) <= off + U[dtype][0] * (np.abs(out) + off)).all()
+
+
+def test_sine_and_cosine_in_32_bits():
+    """Of rows whose pairs are (1, 0), which come out as the cosine and the sine themselves.  They carry their own rounding, E / 2 of at most 1,
+    and that of the last operation, E / 2, and E at the most for the reduced angle and the series between them."""
+    n = 20000
+    pos = torch.randint(-2_000_000, 2_000_000, (1, n), generator=torch.Generator().manual_seed(5), dtype=torch.int32)
+    q = torch.zeros(1, 1, n, 128, device=DEV)
+    q[..., :64] = 1
+    f = (10000.0 ** (-torch.arange(0, 128, 2, dtype=torch.float64) / 128)).float()
+    out = torch.empty_like(q)
+    desc = P.make_rope_desc(batch=1, n_q_heads=1, n_kv_heads=0, head_dim=128, len=n, dtype=P.FP32)
+    P.qk_rope_fwd(desc, q, None, None, None, f.to(DEV), pos.to(DEV), out, None)
+    angle = pos[0].double()[:, None] * f.double()
+    off = (out[0, 0].double().cpu() - torch.cat((angle.cos(), angle.sin()), -1)).abs()
+    assert off.max() <= 2 * E, off.max() / E
