@@ -6,8 +6,26 @@ build module, and that fails if it has not been built (python -m paper_2406_1848
 there is no fallback implementation.
 """
 import importlib
+import types
 
 _LAZY_SUBMODULES = ("binding", "ring", "build")
+
+
+class _Binding(types.ModuleType):
+    """The binding, whose names the package has too: one that is replaced or deleted here is looked up anew there."""
+
+    def __setattr__(self, name, value):
+        _forget(name, self.__dict__.get(name))
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        _forget(name, self.__dict__.get(name))
+        super().__delattr__(name)
+
+
+def _forget(name, value):
+    if value is not None and globals().get(name) is value:
+        del globals()[name]
 
 
 def __getattr__(name):
@@ -20,6 +38,7 @@ def __getattr__(name):
         value = getattr(binding, name)
     except AttributeError:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}") from None
-    if callable(value):   # found once: this search is 4 to 10 us, as much as the rest of a call
+    if callable(value):   # kept: this search is 4 to 10 us, as much as the rest of a call
+        binding.__class__ = _Binding
         globals()[name] = value
     return value
