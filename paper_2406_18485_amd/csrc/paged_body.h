@@ -11,6 +11,10 @@
 namespace loong {
 
 constexpr float kRescaleSlack = 8.f;   // the running maximum may lag the true one by 2^8
+// What is kept is the maximum less so much (log2): the largest probability is then 2^kRaise to 2^(kRaise + kRescaleSlack).  In half, whose
+// steps end at 2^-24, 2^7: 10^5 keys of 2^-25 of the largest one's probability would else be lost from the product together, and not from the sum.
+template <class E>
+constexpr float kRaise = E::code == LOONG_FP16 ? 7.f : 0.f;
 
 typedef __attribute__((address_space(3))) void lds_void_t;
 
@@ -117,7 +121,7 @@ __device__ __forceinline__ void make_finite(unsigned char* piece, int j0, int* o
 // ---- one tile of BNS keys for a wave's 32 rows ------------------------------------------------------------------
 template <int D>
 struct RowState {
-  float m, l;               // maximum (log2 units), this half's sum
+  float m, l;               // maximum less kRaise (log2 units), this half's sum
   floatx16_t o[D / 32];     // O^T
   __device__ __forceinline__ void clear() {
     m = -INFINITY; l = 0.f;
@@ -194,7 +198,7 @@ __device__ __forceinline__ void softmax(const floatx16_t (&s)[NJB], float c, Row
 #pragma unroll
     for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[jb][v]);
   mx = max_with_other_half(mx);
-  const float m_cand = mx * c;
+  const float m_cand = fmaf(mx, c, -kRaise<E>);
   if (__builtin_amdgcn_ballot_w64(m_cand > st.m + kRescaleSlack) != 0) {
     const float m_new = fmaxf(st.m, m_cand);
     const float alpha = m_new == -INFINITY ? 1.f : fast_exp2(st.m - m_new);

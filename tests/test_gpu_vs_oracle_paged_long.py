@@ -156,3 +156,36 @@ def test_queries_of_a_sequence_whose_length_is_negative_are_rotated_as_with_none
     assert all(torch.equal(x, got[0]) for x in got)
     want = ro.rope_forward(f64(c.q)[:4], None, 0.0, np.arange(-4, 0)[:, None], f64(f), False, False)
     assert np.abs(f64(got[0])[:4] - want).max() <= 2.0 ** -8 * np.abs(want).max() + 1e-5
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new,hq,hkv", [(1, 8, 1), (7, 8, 2), (300, 4, 1), (1100, 32, 4)])
+def test_many_small_probabilities_beside_a_large_one(new, hq, hkv, d, dtype):
+    """One key that takes nearly all, and some 10^5 whose probabilities, 2^-23 to 2^-27 of its, have a per cent together.
+
+    A probability's rounding is u of itself, or half a step below the type's normal numbers: half, 2^-25, where the largest is 2^7 at least.
+    The rest of the bound is that of the short calls."""
+    kv = 120000
+    c = Case([new], [kv], dtype=dtype, hq=hq, hkv=hkv, d=d, page=64, clean=True, seed=11)
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    pages, slots = torch.tensor(c.table_np[0, np.arange(kv) // 64], device=DEV), torch.arange(kv, device=DEV) % 64
+    # q all ones but for a little; scores of -0.5 to 0.5 a key, and one of 17 (log2: 24.5)
+    c.q.copy_(1 + 0.01 * torch.randn(c.q.shape, device=DEV, generator=gen))
+    keys = 0.3 * torch.randn(kv, hkv, d, device=DEV, generator=gen)
+    keys -= keys.mean(-1, keepdim=True)
+    keys += (torch.rand(kv, hkv, 1, device=DEV, generator=gen) - 0.5) / (d * c.scale)
+    keys[kv // 3] = 17.0 / (d * c.scale)
+    c.k_cache[pages, :, slots] = keys.to(TORCH[dtype])
+    values = 1 + 0.1 * torch.randn(kv, hkv, d, device=DEV, generator=gen)
+    values[kv // 3] = 0
+    c.v_cache[pages, :, slots] = values.to(TORCH[dtype])
+    c.run()
+    out, lse, size = reference_on_gpu(c)
+    assert 1e-3 < out.mean() < 2e-2
+    u = U[dtype][0]
+    dot = c.scale * 1.01 * (c.q.double().norm(dim=-1).max() * keys.double().norm(dim=-1).max()).item()
+    noise = (2 * kv + 64) * E + 2 * d * E * dot
+    off = (u + noise) * size + (kv * 2.0 ** -32 * 1.6 if dtype == P.FP16 else 0)      # (|v| below 1.6)
+    assert ((c.out.double() - out).abs() <= off).all(), ((c.out.double() - out).abs() / off).max()
+    assert ((c.lse.double() - lse).abs() <= noise + 2 * E * lse.abs()).all()
