@@ -189,9 +189,12 @@ __device__ __forceinline__ void scores(const unsigned char* Kt, const Reads& rd,
   });
 }
 
-// online softmax with a lagging maximum; P^T as operand fragments
-template <class E, int D, int NJB>
-__device__ __forceinline__ void softmax(const floatx16_t (&s)[NJB], float c, RowState<D>& st, uint4 (&pk)[NJB][2]) {
+// online softmax with a lagging maximum; P^T as operand fragments, in one piece or in two: what the storage type holds of a probability,
+// and what it holds of the rest.  Two leave o no further from 64 bits than its own rounding is (one: 1.35 times as far).  Few rows, whose
+// matrix cores are idle for most of the time, have two: one sequence of 1000 keys 12.2 -> 12.7 us, 48 of up to 8192 137.5 -> 138.9.  Many
+// rows have one, as the forward step: 2048 tokens over 32768 keys would be 1026 -> 1411 us.
+template <class E, int D, int NJB, int PIECES>
+__device__ __forceinline__ void softmax(const floatx16_t (&s)[NJB], float c, RowState<D>& st, uint4 (&pk)[PIECES][NJB][2]) {
   float mx = s[0][0];
 #pragma unroll
   for (int jb = 0; jb < NJB; ++jb)
@@ -216,24 +219,37 @@ __device__ __forceinline__ void softmax(const floatx16_t (&s)[NJB], float c, Row
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       e[v] = fast_exp2(fmaf(s[jb][v], c, -m_use));
-      st.l += e[v];   // (P is rounded to the storage type for its product only)
+      st.l += e[v];   // (the sum is of P before it is rounded)
     }
 #pragma unroll
-    for (int sl = 0; sl < 2; ++sl)
-      pk[jb][sl] = make_uint4(E::pack2(e[8 * sl + 0], e[8 * sl + 1]), E::pack2(e[8 * sl + 2], e[8 * sl + 3]),
-                              E::pack2(e[8 * sl + 4], e[8 * sl + 5]), E::pack2(e[8 * sl + 6], e[8 * sl + 7]));
+    for (int piece = 0; piece < PIECES; ++piece)
+#pragma unroll
+      for (int sl = 0; sl < 2; ++sl) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float &x = e[8 * sl + 2 * i], &y = e[8 * sl + 2 * i + 1];
+          w[i] = E::pack2(x, y);
+          if (piece + 1 < PIECES) { x -= E::lo(w[i]); y -= E::hi(w[i]); }
+        }
+        pk[piece][jb][sl] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
   }
 }
 
 // O^T += V^T P^T
-template <class E, int D, int NJB, class Reads>
-__device__ __forceinline__ void values(const unsigned char* Vt, const Reads& rd, const uint4 (&pk)[NJB][2], RowState<D>& st) {
+template <class E, int D, int NJB, int PIECES, class Reads>
+__device__ __forceinline__ void values(const unsigned char* Vt, const Reads& rd, const uint4 (&pk)[PIECES][NJB][2], RowState<D>& st) {
 #pragma unroll
   for (int jb = 0; jb < NJB; ++jb)
 #pragma unroll
     for (int sl = 0; sl < 2; ++sl)
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) st.o[db] = E::mfma(v_frag<D>(Vt, rd, jb, sl, db), as_bf16x8(pk[jb][sl]), st.o[db]);
+      for (int db = 0; db < D / 32; ++db) {
+        const bf16x8_t v = v_frag<D>(Vt, rd, jb, sl, db);
+#pragma unroll
+        for (int piece = 0; piece < PIECES; ++piece) st.o[db] = E::mfma(v, as_bf16x8(pk[piece][jb][sl]), st.o[db]);
+      }
 }
 
 // What the lane's row gets from values of keys [from, to) that are not finite and were left out.

@@ -1,6 +1,6 @@
 // Paged attention of few rows: up to 32 query rows of a kv head (one new token, or a few drafted ones).
 //
-// Bound by HBM, 2 e head_dim bytes a key: the 16 matrix instructions of 32 keys, for 32 rows however few there are, keep a SIMD for 512
+// Bound by HBM, 2 e head_dim bytes a key: the 24 matrix instructions of 32 keys, for 32 rows however few there are, keep a SIMD for 768
 // clocks, and a unit's share of the memory's rate needs 1000 for their 16 KB.  Every wave has tiles of keys and LDS of its own and waits for nobody;
 // while one of its K and V tiles is used the other is on its way: 8 waves a unit keep 64 to 128 KB in flight.
 //
@@ -26,6 +26,7 @@ namespace loong {
 namespace {
 
 constexpr int kFewWaves = 4, kFewPerCu = 2;
+constexpr int kPieces = 2;             // of a probability, see softmax()
 constexpr int kFewFan = 64;            // parts that are added up at a time
 constexpr int kFewLevels = 4;          // 64^4 parts are more than there are shares
 constexpr int kGrain = 64;             // keys that are not divided
@@ -235,15 +236,15 @@ __device__ __forceinline__ void few_keys(const PagedParams& p, const Unit& u, in
         issue_k();
       }
       if (masked) mask_scores<NJB>(s, j0, min(limit, w1), hh);
-      uint4 pk[NJB][2];
-      softmax<E, D, NJB>(s, p.c, st, pk);
+      uint4 pk[kPieces][NJB][2];
+      softmax<E, D, NJB, kPieces>(s, p.c, st, pk);
       if (more) wait_loads<C::LI>();
       else wait_loads<0>();
       if (masked) {
 #pragma unroll 1
         for (int i = 0; i < C::LI; ++i) make_finite<E>(Vt + i * 1024 + lane * 16, j0, &odd_from);
       }
-      values<E, D, NJB>(Vt, rd, pk, st);
+      values<E, D, NJB, kPieces>(Vt, rd, pk, st);
       if (more) {
         wait_reads();   // (of V)
         issue_v();

@@ -220,9 +220,9 @@ __device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& 
       floatx16_t s[NJB];
       scores<E, D, NJB, D / 16 * NJB >= 16 ? 6 : 4>(Kt, rd, qf, s);
       if (masked) mask_scores<NJB>(s, j0, min(limit, w1), hh);
-      uint4 pk[NJB][2];
-      softmax<E, D, NJB>(s, p.c, st, pk);
-      values<E, D, NJB>(Kt + C::TILE_B, rd, pk, st);
+      uint4 pk[1][NJB][2];
+      softmax<E, D, NJB, 1>(s, p.c, st, pk);
+      values<E, D, NJB, 1>(Kt + C::TILE_B, rd, pk, st);
     }
   }
   __syncthreads();   // first_bad and odd_from are final, and the tiles have been read

@@ -189,3 +189,17 @@ def test_many_small_probabilities_beside_a_large_one(new, hq, hkv, d, dtype):
     off = (u + noise) * size + (kv * 2.0 ** -32 * 1.6 if dtype == P.FP16 else 0)      # (|v| below 1.6)
     assert ((c.out.double() - out).abs() <= off).all(), ((c.out.double() - out).abs() / off).max()
     assert ((c.lse.double() - lse).abs() <= noise + 2 * E * lse.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16])
+@pytest.mark.parametrize("new,kv,hq,hkv,d,page", [([1], [1000], 8, 8, 128, 16), ([1, 1, 1], [300, 4000, 7], 16, 2, 64, 24), ([5, 3], [4000, 900], 12, 2, 128, 32),
+                                                  ([1, 2], [30000, 17], 8, 1, 128, 64)])
+def test_few_rows_keep_both_pieces_of_a_probability(new, kv, hq, hkv, d, page, dtype):
+    """The second piece rounds what the first leaves: u of u of sum p|v|/l (half: and 2^-25 of what is 2^7 at least)."""
+    c = Case(new, kv, dtype=dtype, hq=hq, hkv=hkv, d=d, page=page, clean=True, seed=13).run()
+    out, lse, size = reference_on_gpu(c)
+    u = U[dtype][0]
+    dot = c.scale * 1.01 * (c.q.double().norm(dim=-1).max() * c.k_cache.double().nan_to_num().norm(dim=-1).max()).item()
+    noise = (2 * max(kv) + 64) * E + 2 * d * E * dot
+    off = (u * u + noise) * size + (max(kv) * 2.0 ** -32 * c.v_cache.double().nan_to_num().abs().max() if dtype == P.FP16 else 0)
+    assert ((c.out.double() - out).abs() <= off).all(), ((c.out.double() - out).abs() / off).max()
