@@ -203,3 +203,23 @@ def test_few_rows_keep_both_pieces_of_a_probability(new, kv, hq, hkv, d, page, d
     noise = (2 * max(kv) + 64) * E + 2 * d * E * dot
     off = (u * u + noise) * size + (max(kv) * 2.0 ** -32 * c.v_cache.double().nan_to_num().abs().max() if dtype == P.FP16 else 0)
     assert ((c.out.double() - out).abs() <= off).all(), ((c.out.double() - out).abs() / off).max()
+
+
+@pytest.mark.parametrize("new", [[1] * 4200, [1] * 4197 + [0, 70, 2], [0] * 290 + [1, 0, 2, 0, 0, 3, 0, 0, 1, 0], [0] * 290 + [40, 0, 2, 0, 0, 3, 0, 0, 1, 0]])
+def test_thousands_of_sequences(new):
+    """More than a wave has lanes for 64 at a time; and more than there are tokens."""
+    rng = np.random.default_rng(14)
+    kv = [int(rng.integers(1, 100)) if n == 1 else n + int(rng.integers(0, 60)) for n in new]
+    c = Case(new, kv, hq=2, hkv=1, d=64, seed=15).run().check()
+    gen = torch.Generator().manual_seed(16)
+    # and appended: every sequence's tokens are found
+    k, v = (torch.randn(c.tokens, 1, 64, generator=gen).to(torch.bfloat16).to(DEV) for _ in range(2))
+    desc = P.make_paged_desc(n_seqs=len(kv), n_tokens=c.tokens, n_q_heads=2, n_kv_heads=1, head_dim=64, dtype=P.BF16, n_pages=c.n_pages, page_size=16,
+                             max_pages=c.width, table_stride=c.width + 2, rot_dim=0)
+    want_k, want_v = c.k_cache.clone(), c.v_cache.clone()
+    P.paged_append(desc, None, k, v, None, None, None, None, c.seq_start, c.kv_len, c.table, None, c.k_cache, c.v_cache)
+    seq = np.repeat(np.arange(len(new)), new)
+    pos = np.concatenate([np.arange(m - n, m) for n, m in zip(new, kv)])
+    pages, slots = torch.tensor(c.table_np[seq, pos // 16], device=DEV), torch.tensor(pos % 16, device=DEV)
+    want_k[pages, 0, slots], want_v[pages, 0, slots] = k[:, 0], v[:, 0]
+    assert torch.equal(c.k_cache.view(torch.int16), want_k.view(torch.int16)) and torch.equal(c.v_cache.view(torch.int16), want_v.view(torch.int16))
