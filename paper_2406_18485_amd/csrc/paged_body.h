@@ -243,28 +243,68 @@ __device__ __forceinline__ void values(const unsigned char* Vt, const Reads& rd,
 #pragma unroll
   for (int jb = 0; jb < NJB; ++jb)
 #pragma unroll
-    for (int sl = 0; sl < 2; ++sl)
+    for (int sl = 0; sl < 2; ++sl) {
+      if constexpr (PIECES == 1) {
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        const bf16x8_t v = v_frag<D>(Vt, rd, jb, sl, db);
+        for (int db = 0; db < D / 32; ++db) st.o[db] = E::mfma(v_frag<D>(Vt, rd, jb, sl, db), as_bf16x8(pk[0][jb][sl]), st.o[db]);
+      } else {   // (a product does not wait for the one before it)
+        bf16x8_t v[D / 32];
 #pragma unroll
-        for (int piece = 0; piece < PIECES; ++piece) st.o[db] = E::mfma(v, as_bf16x8(pk[piece][jb][sl]), st.o[db]);
+        for (int db = 0; db < D / 32; ++db) v[db] = v_frag<D>(Vt, rd, jb, sl, db);
+#pragma unroll
+        for (int piece = 0; piece < PIECES; ++piece)
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) st.o[db] = E::mfma(v[db], as_bf16x8(pk[piece][jb][sl]), st.o[db]);
       }
+    }
 }
+
+// Four of a key's values, those of a lane's half: f(element, value)
+template <class E, class F>
+__device__ __forceinline__ void four_values(const uint16_t* at, F f) {
+  const uint2 w = *reinterpret_cast<const uint2*>(at);
+  f(0, E::lo(w.x)); f(1, E::hi(w.x)); f(2, E::lo(w.y)); f(3, E::hi(w.y));
+}
+// A key's values of this half (the keys are below cap, so the table has their pages); NULL: a page outside the cache
+__device__ __forceinline__ const uint16_t* values_of(const PagedParams& p, const Unit& s, int key, int hh) {
+  const int idx = (int)page_of(p, key), page = p.table[s.b * p.ts + idx];
+  if ((uint32_t)page >= (uint32_t)p.n_pages) return nullptr;
+  return p.v + page * p.cs[0] + s.hk * p.cs[1] + (key - idx * p.page_size) * p.cs[2] + 4 * hh;
+}
+__device__ __forceinline__ float odd_part(float x) { return x - x == 0.f ? 0.f : x; }
 
 // What the lane's row gets from values of keys [from, to) that are not finite and were left out.
 template <class E, int D>
 __device__ __forceinline__ void add_odd_values(const PagedParams& p, const Unit& s, int from, int to, int hh, RowState<D>& st) {
   for (int key = from; key < to; ++key) {
-    const int idx = (int)page_of(p, key), page = p.table[s.b * p.ts + idx];   // (below cap, so the table has it)
-    if ((uint32_t)page >= (uint32_t)p.n_pages) continue;
-    const uint16_t* row = p.v + page * p.cs[0] + s.hk * p.cs[1] + (key - idx * p.page_size) * p.cs[2] + 4 * hh;
+    const uint16_t* row = values_of(p, s, key, hh);
+    if (!row) continue;
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      const uint2 w = *reinterpret_cast<const uint2*>(row + i * 8);
-      auto add = [&](int e, float x) { st.o[i / 4][4 * (i % 4) + e] += x - x == 0.f ? 0.f : x; };
-      add(0, E::lo(w.x)); add(1, E::hi(w.x)); add(2, E::lo(w.y)); add(3, E::hi(w.y));
+    for (int i = 0; i < D / 8; ++i) four_values<E>(row + i * 8, [&](int e, float x) { st.o[i / 4][4 * (i % 4) + e] += odd_part(x); });
+  }
+}
+// After products with probabilities in two pieces: the second piece may be negative or zero, and makes a NaN of an infinite value.  A row
+// that has a NaN and got no other from its scores looks for such values among its keys [from, to): a column that has any is their sum.
+template <class E, int D>
+__device__ __forceinline__ void settle_odd_values(const PagedParams& p, const Unit& s, int from, int to, int hh, RowState<D>& st) {
+  float any[8] = {};   // (sums: NaN also where infinities of both signs meet; the search does no harm)
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) any[v % 8] += st.o[db][v];
+  const float all = ((any[0] + any[1]) + (any[2] + any[3])) + ((any[4] + any[5]) + (any[6] + any[7]));
+  if (all == all || st.l != st.l) return;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    float sum[16] = {};
+    for (int key = from; key < to; ++key) {
+      const uint16_t* row = values_of(p, s, key, hh);
+      if (!row) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) four_values<E>(row + db * 32 + i * 8, [&](int e, float x) { sum[4 * i + e] += odd_part(x); });
     }
+#pragma unroll
+    for (int v = 0; v < 16; ++v) st.o[db][v] = sum[v] != 0.f ? sum[v] : st.o[db][v];
   }
 }
 

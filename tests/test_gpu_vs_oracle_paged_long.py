@@ -223,3 +223,25 @@ def test_thousands_of_sequences(new):
     pages, slots = torch.tensor(c.table_np[seq, pos // 16], device=DEV), torch.tensor(pos % 16, device=DEV)
     want_k[pages, 0, slots], want_v[pages, 0, slots] = k[:, 0], v[:, 0]
     assert torch.equal(c.k_cache.view(torch.int16), want_k.view(torch.int16)) and torch.equal(c.v_cache.view(torch.int16), want_v.view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new,kv,hq,hkv", [([1], [1000], 8, 2), ([4], [5000], 8, 1), ([1, 3], [40000, 700], 4, 1), ([120], [900], 4, 1)])
+def test_infinite_values_that_rows_see(new, kv, hq, hkv, d, dtype):
+    """In the middle of the context: a column of one, of both signs, of a NaN; all else as it was."""
+    c = Case(new, kv, dtype=dtype, hq=hq, hkv=hkv, d=d, page=32, clean=True, seed=17).run()
+    want = c.out.clone(), c.lse.clone()
+    odd = [(3, 10, "inf"), (3, kv[0] // 2, "inf"), (9, kv[0] // 3, "-inf"), (11, 77, "inf"), (11, kv[0] // 2, "-inf"), (40, 200, "nan"), (41, 0, "inf"), (d - 1, 333, "-inf")]
+    for col, key, x in odd:
+        c.v_cache[int(c.table_np[0, key // c.page]), :, key % c.page, col] = float(x)
+    c.reset()
+    c.run()
+    mine = slice(c.starts[0], c.starts[1])
+    for col, x in ((3, "inf"), (9, "-inf"), (41, "inf"), (d - 1, "-inf")):
+        assert (c.out[mine, :, col] == float(x)).all() and (c.o[mine, :, col] == float(x)).all(), col
+        c.out[mine, :, col] = want[0][mine, :, col]
+    for col in (11, 40):
+        assert torch.isnan(c.out[mine, :, col]).all() and torch.isnan(c.o[mine, :, col]).all(), col
+        c.out[mine, :, col] = want[0][mine, :, col]
+    assert torch.equal(c.out, want[0]) and torch.equal(c.lse, want[1])
