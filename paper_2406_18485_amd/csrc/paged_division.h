@@ -37,7 +37,7 @@ __host__ __device__ inline int key_parts(int paged, int keys) { return paged <= 
 // Sums::longest(): keys of the longest sequence that has rows; tiles(rows, load, units): of one kv head, the row tiles and the keys they go
 // over; spans(rows, inv): spans of 1 / inv keys, of one kv head; rcp(x): 1 / x, a step or so off.
 // (Estimates in floats: an integer division is some 40 instructions, and all this is in front of the first load of a key.)
-template <bool BOTH, int D, class Sums>
+template <bool SMALLER, int D, class Sums>
 __host__ __device__ inline Division choose_division(const Sums& sums, int hkv, const ManyArgs& a) {
   float best = INFINITY;
   const float hold = (float)a.hold, per_place = sums.rcp(hold), slower = hold * sums.rcp((float)a.cus);
@@ -47,7 +47,7 @@ __host__ __device__ inline Division choose_division(const Sums& sums, int hkv, c
   const int whole = whole_tiles(most);
   Division d{256, whole, false};
 #pragma unroll
-  for (int small = 0; small < (BOTH ? 3 : 1); ++small) {
+  for (int small = 0; small < (SMALLER ? 3 : 1); ++small) {
     const int rows = 256 >> small;
     float load, units;
     sums.tiles(rows, load, units);
@@ -96,8 +96,8 @@ inline int64_t most_units(const loong_paged_desc& d, int rows) {
   return ((d.n_seqs < d.n_tokens ? d.n_seqs : d.n_tokens) + d.n_tokens * group / rows) * d.n_kv_heads;
 }
 inline ManyArgs many_args(const loong_paged_desc& d, int cus) {
-  const bool both = !rows_fill(d, cus);
-  return ManyArgs{cus, d.head_dim == 64 && !both ? 2 * cus : cus, (int)most_units(d, both ? 64 : 256)};
+  const bool smaller = !rows_fill(d, cus);
+  return ManyArgs{cus, d.head_dim == 64 && !smaller ? 2 * cus : cus, (int)most_units(d, smaller ? 64 : 256)};
 }
 
 // Where row tiles of 256 fill the chip the hardware deals the spans out, else as many workgroups as it holds take them in turn.
@@ -105,13 +105,13 @@ inline ManyArgs many_args(const loong_paged_desc& d, int cus) {
 // them and a remainder a unit, and at most as many units are cut.
 inline PagedPlan plan_many(const loong_paged_desc& d, int cus) {
   PagedPlan pl{};
-  const bool both = !rows_fill(d, cus);
-  const int64_t units = most_units(d, both ? 64 : 256);
+  const bool smaller = !rows_fill(d, cus);
+  const int64_t units = most_units(d, smaller ? 64 : 256);
   const int64_t keys = cached_keys(d), parts = keys <= kManyLeast ? 1 : (keys + kManyLeast - 1) / kManyLeast;
   const int64_t more = (int64_t)(kManyMore * cus * 1.01) + 8;
   int64_t spans = units + more;
   if (units * parts < spans) spans = units * parts;
-  pl.workgroups = both && spans > cus ? cus : spans;
+  pl.workgroups = smaller && spans > cus ? cus : spans;
   pl.workgroups = (pl.workgroups + 7) / 8 * 8;
   pl.slots = parts == 1 ? 0 : 2 * more < spans ? 2 * more : spans;
   pl.slot_floats = 256 * (d.head_dim + 4);

@@ -345,18 +345,18 @@ __device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& 
   if (ksp == 0 && hh == 0) p.lse[(int64_t)token * p.hq + head] = lse_of(m_all, l_tot);
 }
 
-// BOTH: row tiles of 128 and 64 too; with every unit of the chip holding one workgroup, which goes on from span to span.
-// Else, at head_dim 64, two workgroups a unit fit, in 128 registers and with 68 bytes of scratch memory, of which the loop over
+// SMALLER: row tiles of 128 and 64 too; with every unit of the chip holding one workgroup, which goes on from span to span.
+// Else, at head_dim 64, two workgroups a unit fit, in 128 registers and with 72 bytes of scratch memory, of which the loop over
 // tiles reads one value: 8000 tokens over 30000 keys, 32 heads on 8, 2125 -> 1996 us.  (The other side: 2500 tokens' own prompt, 32 heads of own keys, 320
 // tiles for 256 units, 60 -> 80 us, as the units that hold two end last; over 8000 keys, where tiles are cut, 249 -> 227.)
-template <class E, int D, bool BOTH>
-__global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void paged_many_kernel(const PagedParams p, const ManyArgs a) {
-  constexpr int BYTES = BOTH ? std::max({ManyCfg<D, 1>::SMEM_B, ManyCfg<D, 2>::SMEM_B, ManyCfg<D, 4>::SMEM_B}) : ManyCfg<D, 1>::SMEM_B;
+template <class E, int D, bool SMALLER>
+__global__ __launch_bounds__(kManyWaves * 64, D == 64 && !SMALLER ? 4 : 2) void paged_many_kernel(const PagedParams p, const ManyArgs a) {
+  constexpr int BYTES = SMALLER ? std::max({ManyCfg<D, 1>::SMEM_B, ManyCfg<D, 2>::SMEM_B, ManyCfg<D, 4>::SMEM_B}) : ManyCfg<D, 1>::SMEM_B;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[BYTES];
   __shared__ ManyShared sh;
   const Lanes lanes(p);
   const WaveSums sums{p, lanes};
-  const Division d = choose_division<BOTH, D>(sums, p.hkv, a);
+  const Division d = choose_division<SMALLER, D>(sums, p.hkv, a);
   const int all = sums.all(d);   // spans
   // neighbours share an XCD and its L2 where they read the same keys
   const int per = (all + 7) / 8, xcd = blockIdx.x & 7;
@@ -367,8 +367,8 @@ __global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void pag
     if (item >= all || !find_span(p, d, lanes, item, sp)) break;
     if (again) __syncthreads();   // the span before is done with LDS
     again = true;
-    if (!BOTH || d.rows == 256) many_span<E, D, 1>(p, sp, d.keys, smem, sh);
-    else if constexpr (BOTH) {
+    if (!SMALLER || d.rows == 256) many_span<E, D, 1>(p, sp, d.keys, smem, sh);
+    else if constexpr (SMALLER) {
       if (d.rows == 128) many_span<E, D, 2>(p, sp, d.keys, smem, sh);
       else many_span<E, D, 4>(p, sp, d.keys, smem, sh);
     }
@@ -376,9 +376,9 @@ __global__ __launch_bounds__(kManyWaves * 64, D == 64 && !BOTH ? 4 : 2) void pag
 }
 
 template <class E, int D>
-void launch(const PagedParams& p, bool both, const ManyArgs& a, unsigned grid, hipStream_t st) {
+void launch(const PagedParams& p, bool smaller, const ManyArgs& a, unsigned grid, hipStream_t st) {
   const dim3 g(grid), b(kManyWaves * 64);
-  if (both) paged_many_kernel<E, D, true><<<g, b, 0, st>>>(p, a);
+  if (smaller) paged_many_kernel<E, D, true><<<g, b, 0, st>>>(p, a);
   else paged_many_kernel<E, D, false><<<g, b, 0, st>>>(p, a);
 }
 
@@ -388,14 +388,14 @@ PagedPlan plan_paged_many(const loong_paged_desc& d, int cus) { return plan_many
 
 void launch_paged_many(const PagedParams& p, const loong_paged_desc& d, int cus, unsigned grid, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool both = !rows_fill(d, cus);
+  const bool smaller = !rows_fill(d, cus);
   const ManyArgs a = many_args(d, cus);
   if (d.dtype == LOONG_BF16) {
-    if (d.head_dim == 128) launch<Bf16, 128>(p, both, a, grid, st);
-    else launch<Bf16, 64>(p, both, a, grid, st);
+    if (d.head_dim == 128) launch<Bf16, 128>(p, smaller, a, grid, st);
+    else launch<Bf16, 64>(p, smaller, a, grid, st);
   } else {
-    if (d.head_dim == 128) launch<Fp16, 128>(p, both, a, grid, st);
-    else launch<Fp16, 64>(p, both, a, grid, st);
+    if (d.head_dim == 128) launch<Fp16, 128>(p, smaller, a, grid, st);
+    else launch<Fp16, 64>(p, smaller, a, grid, st);
   }
 }
 

@@ -56,9 +56,9 @@ extern "C" void divide(const loong_paged_desc* d, int cus, int ulps, const int32
     seqs.push_back({(n_new[b] < d->max_new ? n_new[b] : d->max_new) * (d->n_q_heads / d->n_kv_heads), (int)(kv[b] < cap ? kv[b] : cap)});
   const HostSums sums{seqs, ulps};
   const ManyArgs a = many_args(*d, cus);
-  const bool both = !rows_fill(*d, cus);
-  const Division r = d->head_dim == 128 ? (both ? choose_division<true, 128>(sums, d->n_kv_heads, a) : choose_division<false, 128>(sums, d->n_kv_heads, a))
-                                        : (both ? choose_division<true, 64>(sums, d->n_kv_heads, a) : choose_division<false, 64>(sums, d->n_kv_heads, a));
+  const bool smaller = !rows_fill(*d, cus);
+  const Division r = d->head_dim == 128 ? (smaller ? choose_division<true, 128>(sums, d->n_kv_heads, a) : choose_division<false, 128>(sums, d->n_kv_heads, a))
+                                        : (smaller ? choose_division<true, 64>(sums, d->n_kv_heads, a) : choose_division<false, 64>(sums, d->n_kv_heads, a));
   int64_t all = 0, cut = 0, most = 0;
   for (auto& s : seqs) {
     if (r.none || r.keys <= 0 || s.rows == 0) continue;
