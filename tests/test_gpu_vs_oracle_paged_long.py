@@ -245,3 +245,60 @@ def test_infinite_values_that_rows_see(new, kv, hq, hkv, d, dtype):
         assert torch.isnan(c.out[mine, :, col]).all() and torch.isnan(c.o[mine, :, col]).all(), col
         c.out[mine, :, col] = want[0][mine, :, col]
     assert torch.equal(c.out, want[0]) and torch.equal(c.lse, want[1])
+
+
+@pytest.mark.parametrize("new,kv,hq,d", [([40], [200000], 1, 64), ([40], [100000], 1, 128), ([260], [200000], 1, 128), ([40, 1], [100000, 300], 1, 64), ([900], [80000], 8, 64),
+                                         ([33], [30000], 1, 64)])
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16])
+def test_many_rows_whose_parts_are_added_up_in_several_levels(new, kv, hq, d, dtype):
+    """241, 224, 51, 121, 8 and 118 parts of a unit on a chip of 256 units, four at a time: two to four levels."""
+    check(Case(new, kv, dtype=dtype, hq=hq, hkv=1, d=d, page=48, clean=True, seed=18).run())
+
+
+def test_many_rows_replayed_between_divisions():
+    c = Case([60, 40], [100000, 40000], hq=2, hkv=1, d=64, page=64, clean=True, seed=19)
+    lengths = [[100000, 40000], [60, 40000], [100000, 40], [300, 200], [4000, 90], [59, 0], [100000, 39999]]
+    want = []
+    for kv in lengths:
+        c.kv_len.copy_(torch.tensor(kv, dtype=torch.int32))
+        c.reset()
+        c.run()
+        want.append((c.out.clone(), c.lse.clone()))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.run()
+    for _ in range(2):
+        for kv, (out, lse) in zip(lengths, want):
+            c.kv_len.copy_(torch.tensor(kv, dtype=torch.int32))
+            c.out.fill_(3.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
+            assert (c.ws[:P.WORKSPACE_HEAD] == 0).all()
+
+
+def test_one_workspace_for_calls_of_both_kinds():
+    """Few rows, many rows and few again, in one captured step, with counters that nobody clears."""
+    few = Case([1, 2], [30000, 4000], hq=8, hkv=2, d=64, page=64, clean=True, seed=20)
+    many = Case([300, 40], [30000, 4000], hq=8, hkv=2, d=64, page=64, clean=True, seed=21)
+    want = []
+    for c in (few, many):
+        c.run()
+        want.append((c.out.clone(), c.lse.clone()))
+    ws = few.ws if few.ws.numel() > many.ws.numel() else many.ws
+    few.ws = many.ws = ws.zero_()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for c in (few, many, few):
+            c.run()
+    for _ in range(3):
+        for c in (few, many):      # (the captured calls' own tensors)
+            c.out.fill_(3.0)
+            c.lse.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for c, (out, lse) in zip((few, many), want):
+            assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
+        assert (ws[:P.WORKSPACE_HEAD] == 0).all()
