@@ -283,8 +283,9 @@ __device__ __forceinline__ void add_odd_values(const PagedParams& p, const Unit&
     for (int i = 0; i < D / 8; ++i) four_values<E>(row + i * 8, [&](int e, float x) { st.o[i / 4][4 * (i % 4) + e] += odd_part(x); });
   }
 }
-// After products with probabilities in two pieces: the second piece may be negative or zero, and makes a NaN of an infinite value.  A row
-// that has a NaN and got no other from its scores looks for such values among its keys [from, to): a column that has any is their sum.
+// Infinite values are multiplied like others where every row sees them.  A probability that is zero in the storage type, or a second piece
+// that is zero or negative, makes a NaN of them: a row that has one, and got no other from its scores, looks for such values among its
+// keys [from, to), and a column that has any is their sum.
 template <class E, int D>
 __device__ __forceinline__ void settle_odd_values(const PagedParams& p, const Unit& s, int from, int to, int hh, RowState<D>& st) {
   float any[8] = {};   // (sums: NaN also where infinities of both signs meet; the search does no harm)

@@ -225,6 +225,7 @@ __device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& 
       values<E, D, NJB, 1>(Kt + C::TILE_B, rd, pk, st);
     }
   }
+  settle_odd_values<E, D>(p, u, k0, min(limit, k1), hh, st);
   __syncthreads();   // first_bad and odd_from are final, and the tiles have been read
   if (limit > first_bad) st.l = NAN;
   if (ksp == 0) add_odd_values<E, D>(p, u, odd_from, min(limit, k1), hh, st);   // (behind a masked tile all are)

@@ -302,3 +302,26 @@ def test_one_workspace_for_calls_of_both_kinds():
         for c, (out, lse) in zip((few, many), want):
             assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
         assert (ws[:P.WORKSPACE_HEAD] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new,hq", [([1], 4), ([100], 1), ([300], 8)])
+def test_infinite_values_of_keys_with_hardly_any_weight(new, hq, d, dtype):
+    """2^-40 of the largest, nothing in half: the result is infinite all the same."""
+    kv = [new[0] + 400]
+    c = Case(new, kv, dtype=dtype, hq=hq, hkv=1, d=d, page=32, clean=True, seed=22)
+    c.q.fill_(1.0)
+    place = lambda key: (int(c.table_np[0, key // c.page]), slice(None), key % c.page)
+    for key in range(kv[0]):
+        c.k_cache[place(key)] = 28.0 / (d * c.scale) if key == 1 else 0.0
+    c.run()
+    want = c.out.clone(), c.lse.clone()
+    for key, col, x in ((5, 5, "inf"), (9, 33, "-inf"), (13, 40, "nan")):   # (the same tile, so that the largest counts)
+        c.v_cache[(*place(key), col)] = float(x)
+    c.reset()
+    c.run()
+    assert (c.out[..., 5] == float("inf")).all() and (c.out[..., 33] == float("-inf")).all() and torch.isnan(c.out[..., 40]).all()
+    for col in (5, 33, 40):
+        c.out[..., col] = want[0][..., col]
+    assert torch.equal(c.out, want[0]) and torch.equal(c.lse, want[1])
