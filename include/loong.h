@@ -379,7 +379,9 @@ LOONG_API int loong_paged_append(const loong_paged_desc* desc, const void* q, co
  * Long contexts of few rows are shared by several workgroups; which, follows from the lengths, and the last to arrive adds
  * their results up in order: the same lengths give the same bits.  Their results and counters live in `workspace`, 16-byte aligned, of
  * loong_paged_workspace_bytes(desc) bytes (that may be 0: then it may be NULL); contents, order and LOONG_WORKSPACE_CLEAN as for
- * loong_attn_step_bwd.  What a masked key or value holds, be it infinite or NaN, has no effect.
+ * loong_attn_step_bwd.  What a masked key or value holds, be it infinite or NaN, has no effect; an infinite or NaN value that a row sees makes its
+ * column of that row infinite or NaN, however little weight it has.  For its product with the values a probability is rounded to dtype, or, where no
+ * sequence has more than 32 rows of a kv head, to the sum of two numbers of dtype.
  */
 LOONG_API int loong_paged_attn(const loong_paged_desc* desc, const void* q, const void* k_cache, const void* v_cache,
                                const int32_t* seq_start, const int32_t* kv_len, const int32_t* page_table, float* out, void* o,

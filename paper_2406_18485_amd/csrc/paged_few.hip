@@ -15,7 +15,7 @@
 // over the whole chip are not read by one workgroup.  (Two contexts of 262144 keys, one kv head: 127 us with 512 parts added up by
 // one workgroup, 77 sixteen at a time.  A further level costs 5 us: 16000 keys of 8 heads, 62 parts, 22.5 us in two, 20.3 in one.)
 //
-// 48 sequences, 708 MB of keys and values: 137 us, 5.2 TB/s (64 of 4000 keys 5.6).  The shortest call, one sequence of up to 32 keys, takes 7.4 us, a launch
+// 48 sequences, 708 MB of keys and values: 138 us, 5.1 TB/s (64 of 4000 keys 5.6).  The shortest call, one sequence of up to 32 keys, takes 7.8 us, a launch
 // alone 2.3: the rest is the chain of loads lengths -> page numbers -> keys, a microsecond each, and the sums over waves; an
 // exchange adds 3.5.
 #include <hip/hip_runtime.h>
