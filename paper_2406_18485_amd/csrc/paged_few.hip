@@ -251,7 +251,7 @@ __device__ __forceinline__ void few_keys(const PagedParams& p, const Unit& u, in
       }
     }
   }
-  settle_odd_values<E, D>(p, u, k0, min(limit, k1), hh, st);
+  settle_odd_values<E, D>(p, u, k0, min(limit, k1), hh, st, reinterpret_cast<floatx4_t*>(Kt));   // (the wave's tiles are used up)
 }
 
 // The waves' results, and those of the unit's other parts.

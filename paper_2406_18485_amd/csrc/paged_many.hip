@@ -225,8 +225,10 @@ __device__ __forceinline__ void many_span(const PagedParams& p, const ManySpan& 
       values<E, D, NJB, 1>(Kt + C::TILE_B, rd, pk, st);
     }
   }
-  settle_odd_values<E, D>(p, u, k0, min(limit, k1), hh, st);
   __syncthreads();   // first_bad and odd_from are final, and the tiles have been read
+  static_assert(KS > 1 || C::SMEM_B >= kManyWaves * 128 * D, "a wave's results fit into its part of the tiles");
+  // (where splits are combined, that is the place this wave puts its results in afterwards)
+  settle_odd_values<E, D>(p, u, k0, min(limit, k1), hh, st, reinterpret_cast<floatx4_t*>(smem) + wave * (KS > 1 ? C::SLOT_F4 * 64 : 8 * D));
   if (limit > first_bad) st.l = NAN;
   if (ksp == 0) add_odd_values<E, D>(p, u, odd_from, min(limit, k1), hh, st);   // (behind a masked tile all are)
 

@@ -325,3 +325,20 @@ def test_infinite_values_of_keys_with_hardly_any_weight(new, hq, d, dtype):
     for col in (5, 33, 40):
         c.out[..., col] = want[0][..., col]
     assert torch.equal(c.out, want[0]) and torch.equal(c.lse, want[1])
+
+
+@pytest.mark.parametrize("dtype", [P.BF16, P.FP16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [2, 200])
+def test_values_that_are_none_of_them_finite(new, d, dtype):
+    """All NaN; all infinite, of one sign in even columns and of both in odd ones."""
+    c = Case([new], [3000], dtype=dtype, hq=4, hkv=1, d=d, page=32, clean=True, seed=23).run()
+    lse = c.lse.clone()
+    for what in ("nan", "inf"):
+        c.v_cache.fill_(float(what))
+        if what == "inf":
+            c.v_cache[:, :, ::2, 1::2] = float("-inf")
+        c.reset()
+        c.run()
+        assert torch.isnan(c.out[..., 1::2]).all() and torch.equal(c.lse, lse)
+        assert torch.isnan(c.out[..., ::2]).all() if what == "nan" else (c.out[..., ::2] == float("inf")).all()
